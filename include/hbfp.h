@@ -688,6 +688,136 @@ int hbfp_weight_update(const hbfp_tensor *wide, const float *delta, int64_t ld, 
 int hbfp_probe_matrix_rate(int instruction, const int *words, int workgroups, int iters, float *sink, long long *clocks,
                            void *stream);
 
+/*
+ * ---- Serving: a cache of keys and values in 4-bit BFP, the attention that reads it, eviction from it
+ *
+ * The cache holds keys and values as the conversion rule above writes them with 4-bit mantissas: blocks of 32 values along
+ * the head dimension share one exponent byte Eb, mantissas are round-to-nearest-even integers in +-7, one unit is worth
+ * 2^(Eb - 129).  4.25 bits a value.  Everything that reads the cache is defined on the values it holds.
+ *
+ * hbfp_cache_plan fills everything but the four pointers; the caller sets those (device, 16-byte aligned).  `slots` is the
+ * capacity rounded up to 64: the buffers hold that many tokens a head, so that kernels may load whole groups.  Per (batch,
+ * head), nblk = ceil(dim / 32); values past dim are stored as 0:
+ *   k       [slots][4 g][nblk][4 y]       byte y: dimension 32 blk + 8 g + y (low nibble) and + 4 (high nibble)
+ *   v       [slots / 4][16 c][nblk][4 j]  byte j: slot 4 group + j, dimensions 32 blk + c (low nibble) and + 16 (high nibble)
+ *   *_exps  [slots / 4][nblk][4 j]        exponent byte of slot 4 group + j
+ * A nibble is the magnitude with the sign above it.  Slots that were never written may hold anything.
+ *
+ * `lengths` (device, int32 per batch entry) is always the number of tokens the cache holds AFTER the call's new tokens: token
+ * t of `tokens` belongs to slot lengths[b] - tokens + t.  A batch entry with fewer new tokens than `tokens` is padded on the
+ * left: its first tokens get negative slots, which nothing stores or sees.  Slots from the capacity on do not exist: their
+ * tokens are not stored, and nothing sees them.  A negative length is read as 0.
+ *
+ * Tensors of one call's tokens, [batch][tokens][heads][dim], are given as hbfp_heads: dim is contiguous, the other strides are
+ * free (slices of one projection; an input may be broadcast with stride 0).  Types: HBFP_F32, HBFP_BF16, HBFP_F16.
+ */
+enum { HBFP_F32 = 0, HBFP_BF16 = 1, HBFP_F16 = 2 };
+
+typedef struct hbfp_cache {
+    uint8_t *k, *v;              /* device, code_bytes each, 16-byte aligned */
+    uint8_t *k_exps, *v_exps;    /* device, exp_bytes each, 16-byte aligned */
+    int64_t batch, heads, capacity, dim;
+    int64_t slots, nblk;
+    uint64_t code_bytes, exp_bytes;
+} hbfp_cache;
+
+typedef struct hbfp_heads {
+    void *data;                  /* device; element (b, t, h, d) at b * stride_batch + t * stride_token + h * stride_head + d */
+    int32_t dtype;               /* HBFP_F32, HBFP_BF16 or HBFP_F16 */
+    int32_t reserved;            /* 0 */
+    int64_t stride_batch, stride_token, stride_head;   /* in elements, not negative */
+} hbfp_heads;
+
+/*
+ * hbfp_cache_plan (host only): geometry and byte sizes.  heads: key/value heads; dim 1..256.
+ * Errors: HBFP_ERR_ARG (null, sizes <= 0), HBFP_ERR_FORMAT (dim > 256, or a head's buffer of 2^31 bytes and more).
+ */
+int hbfp_cache_plan(int64_t batch, int64_t heads, int64_t capacity, int64_t dim, hbfp_cache *out);
+
+/*
+ * hbfp_cache_append: converts the new tokens' keys and values and stores them.  k_values, v_values (each may be NULL): bf16
+ * [batch][tokens][heads][dim], contiguous, receive the values the cache now holds for them (exact in bf16), 0 for tokens that
+ * were not stored.  Inputs must be finite and below 2^127; a block with an Inf or a NaN makes what reads it NaN or Inf.
+ * Errors: HBFP_ERR_ARG, HBFP_ERR_FORMAT (dtype), HBFP_ERR_LAYOUT (cache differs from its plan), HBFP_ERR_LAUNCH.
+ */
+int hbfp_cache_append(const hbfp_cache *cache, const hbfp_heads *k, const hbfp_heads *v, int64_t tokens, const int32_t *lengths,
+                      void *k_values, void *v_values, void *stream);
+
+/*
+ * hbfp_cache_read: the values the cache holds, [batch][heads][capacity][dim] contiguous, in FP32 or bf16 (exact in both); 0
+ * from a batch entry's length on.  k or v may be NULL.
+ */
+int hbfp_cache_read(const hbfp_cache *cache, const int32_t *lengths, int dtype, void *k, void *v, void *stream);
+
+/*
+ * hbfp_cache_attend: softmax attention of the new tokens' queries over the cache.
+ *   q, out   [batch][tokens][heads][dim], one type; heads a multiple of cache->heads: query head h reads key head
+ *            h / (heads / cache->heads)
+ *   s[j] = scale * q . k[j];  visible keys: j <= slot of the query's own token if causal, else j < lengths[b];
+ *   lse  [batch][tokens][heads] FP32: log(sum exp(s)) over the visible keys;  out = sum exp(s - lse) v
+ *   A query that sees no key: out = 0, lse = -infinity.  Masked keys and values have no influence, whatever they hold.
+ *   longest  the caller's bound on the lengths (it sizes the launch); 0 = the capacity.  Keys from it on are not seen.
+ * The scores, the softmax statistics and the sums are FP32.  bf16 queries enter the products exactly and the weights exp(s - max)
+ * rounded to bf16; FP16 queries exactly and the weights as two bf16 numbers (16 bits); FP32 both as three (24 bits).
+ * workspace: hbfp_cache_attend_workspace bytes, 256-byte aligned.  Errors: as hbfp_cache_append, HBFP_ERR_WORKSPACE.
+ */
+int hbfp_cache_attend_workspace(const hbfp_cache *cache, int64_t tokens, int64_t heads, int dtype, int64_t longest, size_t *bytes);
+int hbfp_cache_attend(const hbfp_cache *cache, const hbfp_heads *q, int64_t tokens, int64_t heads, const int32_t *lengths,
+                      int64_t longest, float scale, int causal, const hbfp_heads *out, float *lse, void *workspace, size_t ws_bytes,
+                      void *stream);
+
+/*
+ * hbfp_cache_weigh: the attention weight every cached token received, accumulated:
+ *   w_out[b][h][j] = decay * w_in[b][h][j] + sum over the call's tokens and the query heads of key head h of exp(s[j] - lse)
+ * for j < lengths[b], 0 for j from there to the capacity.  q, tokens, heads, lengths, scale, causal and lse as in (and from)
+ * hbfp_cache_attend; w_in and w_out are FP32 [batch][cache->heads][ld], ld >= capacity; w_out may be w_in.
+ */
+int hbfp_cache_weigh(const hbfp_cache *cache, const hbfp_heads *q, int64_t tokens, int64_t heads, const int32_t *lengths, float scale,
+                     int causal, const float *lse, float decay, const float *w_in, float *w_out, int64_t ld, void *stream);
+
+/*
+ * hbfp_cache_evict: copies of every head the tokens that matter into another cache (one spare cache serves all layers of a
+ * network in turn), in their order, and packs their weights likewise.  A batch entry of n > keep tokens keeps its last
+ * r = min(recent, keep) and, of the others, the keep - r with the largest weights (equal weights: lowest slot first; a NaN
+ * counts as the lowest); one of n <= keep tokens keeps all.  Each head chooses for itself.
+ *   w, w_out     FP32 [batch][heads][ld], ld >= src->capacity, and [batch][heads][ld_out], ld_out >= dst->capacity; w_out is 0
+ *                from the new length to dst->capacity
+ *   kept         int32 [batch][heads][keep]: the slots that stay, -1 from the new length on
+ *   lengths_out  int32 per batch entry: min(n, keep)
+ * dst: same batch, heads and dim, capacity >= keep; its buffers and w_out may not overlap the inputs.
+ * Errors: HBFP_ERR_ARG, HBFP_ERR_LAYOUT (caches do not fit each other), HBFP_ERR_LAUNCH.
+ */
+int hbfp_cache_evict(const hbfp_cache *src, const float *w, int64_t ld, const int32_t *lengths, int64_t keep, int64_t recent,
+                     const hbfp_cache *dst, float *w_out, int64_t ld_out, int32_t *kept, int32_t *lengths_out, void *stream);
+
+/*
+ * ---- Products in 8-bit integers with an FP32 scale for each token and channel
+ *
+ * A matrix [rows][cols] as rows of codes: row r is codes[r][0..cols-1] * scales[r], int8 codes in +-127, in rows of
+ * kpad = cols rounded up to 128 bytes whose padding is 0 (hbfp_rows_plan gives the sizes).
+ * hbfp_quant_rows: scales[r] = max |x[r]| * (1 / 127), an FP32 product with the FP32 number nearest to 1 / 127; code = x / scale
+ * rounded in FP32, then to the nearest integer, ties to even; a row of zeros has scale 0 and codes 0.  An Inf or a NaN in a row makes its scale Inf or NaN.
+ *   src  [rows][ld], HBFP_F32, HBFP_BF16 or HBFP_F16
+ */
+int hbfp_rows_plan(int64_t rows, int64_t cols, int64_t *kpad, size_t *code_bytes);
+int hbfp_quant_rows(const void *src, int dtype, int64_t rows, int64_t cols, int64_t ld, int8_t *codes, float *scales, void *stream);
+
+/*
+ * hbfp_gemm_rows: Y[m][n] = (sum_k a[m][k] b[n][k]) * a_scales[m] * b_scales[n] + bias[n], the sum an exact int32, the rest FP32
+ * with Y rounded once to its type.  a: M rows (tokens), b: N rows (channels), both of K codes in rows of kpad bytes, 16-byte
+ * aligned.  bias: FP32 [N] or NULL.  y: [M][ldy], ldy >= N.
+ * hbfp_linear_i8: hbfp_quant_rows of x and the product in one call; Y has x's type.
+ * workspace: the matching _workspace bytes, 256-byte aligned.
+ * Errors: HBFP_ERR_ARG, HBFP_ERR_FORMAT (dtype), HBFP_ERR_RANGE (K * 127^2 reaches 2^31: K > 133144), HBFP_ERR_WORKSPACE,
+ * HBFP_ERR_LAUNCH.
+ */
+int hbfp_gemm_rows_workspace(int64_t M, int64_t N, int64_t K, size_t *bytes);
+int hbfp_gemm_rows(const int8_t *a, const float *a_scales, const int8_t *b, const float *b_scales, const float *bias, int64_t M,
+                   int64_t N, int64_t K, void *y, int dtype, int64_t ldy, void *workspace, size_t ws_bytes, void *stream);
+int hbfp_linear_i8_workspace(int64_t M, int64_t N, int64_t K, size_t *bytes);
+int hbfp_linear_i8(const void *x, int dtype, int64_t M, int64_t K, int64_t ldx, const int8_t *b, const float *b_scales,
+                   const float *bias, int64_t N, void *y, int64_t ldy, void *workspace, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,464 @@
+// Softmax attention over the 4-bit cache for few queries per key head (single tokens, drafted tokens), and the accumulation of
+// attention weights.
+//
+// A wave holds 16 queries of one key head (the tokens' queries of the heads that share it) and walks over keys 64 at a time:
+// scores S^T = K Q^T, so that a lane has one query's scores of 16 keys, the running maximum and sum of the softmax, and
+// O^T += V^T P^T, whose second operand is the scores' own register layout: nothing passes through LDS between the two
+// products.  The contraction of the first runs over dimensions, and a key's exponents are applied when its nibbles become bf16
+// numbers; the contraction of the second runs over keys, whose exponents differ, so they multiply the weights, block of 32
+// dimensions by block, and the values enter as integers (n / 4).
+#include "kv_cache.h"
+
+namespace hbfp {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kWaves = 4;
+
+struct SplitParams {
+    AttendArgs a;
+    float *ml, *o;            // partial results: [batch * heads][chunks][rows] (max, sum) and [..][32 nblk]
+    int32_t rows, tiles, chunk, chunks;
+    float scale2;             // scale * log2(e)
+    uint32_t wgs;
+};
+
+// keys that row `row` (token row / group) of batch entry b may see
+__device__ __forceinline__ int visible(int length, int tokens, int group, int row, int causal, int bound) {
+    const int len = length < 0 ? 0 : length;
+    const int64_t n = causal ? (int64_t)len - tokens + row / group + 1 : (int64_t)len;
+    return n < 0 ? 0 : n > bound ? bound : (int)n;
+}
+
+// a wave's 16 queries as the second operand of S^T = K Q^T: lane c + 16 g has dimensions 32 blk + 8 g .. + 7 of query c
+template <int NB, int DT>
+__device__ __forceinline__ void load_queries(const Heads &q, int64_t b, int key_head, int group, int row, int rows, int dim, int g,
+                                             v8bf (&out)[Pieces<DT>::n][NB]) {
+    const bool real = row < rows;
+    const int t = real ? row / group : 0, h = real ? key_head * group + row % group : 0;
+    const int64_t base = b * q.sb + t * q.st + h * q.sh;
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
+        const int d0 = 32 * blk + 8 * g, n = real ? dim - d0 : 0;
+        float x[8];
+        load8<DT>(q.data, base + d0, n, n >= 8 && q.wide, x);
+        uint32_t w[4][Pieces<DT>::n];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bf16_pieces2<Pieces<DT>::n>(x[2 * i], x[2 * i + 1], w[i]);
+#pragma unroll
+        for (int p = 0; p < Pieces<DT>::n; ++p) {
+            const v4u r = {w[0][p], w[1][p], w[2][p], w[3][p]};
+            out[p][blk] = __builtin_bit_cast(v8bf, r);
+        }
+    }
+}
+
+// scores of 16 keys (rows of the result: keys 4 g + i) from 16 g.. of the key layout
+template <int NB, int NP>
+__device__ __forceinline__ v4f scores16(const uint32_t (&w)[NB], const uint32_t (&e)[NB], int j, const v8bf (&q)[NP][NB]) {
+    v4f s = {0, 0, 0, 0};
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
+        const v8bf k = key_values(w[blk], exponent_scale(e[blk], j));
+#pragma unroll
+        for (int p = NP - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[p][blk], s, 0, 0, 0);
+    }
+    return s;
+}
+
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N]) {
+    if (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const v4u x = reinterpret_cast<const v4u *>(p)[i];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[4 * i + k] = x[k];
+        }
+    } else if (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const v2u x = reinterpret_cast<const v2u *>(p)[i];
+            w[2 * i] = x[0];
+            w[2 * i + 1] = x[1];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+    }
+}
+
+// One step of KS keys from key0 on.  MASK: some of the wave's queries do not see all of them.
+template <int NB, int NP, int KS, bool MASK>
+__device__ __forceinline__ void attend_step(const uint8_t *k, const uint8_t *ke, const uint8_t *v, const uint8_t *ve, int key0, int limit,
+                                            float scale2, int c, int g, const v8bf (&q)[NP][NB], v4f (&o)[2 * NB], float &m, float &l) {
+    constexpr int T = KS / 16;
+    uint32_t kw[T][NB], kx[T][NB], vw[T][NB], vx[T][NB];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        const uint32_t key = key0 + 16 * t + c, group = (key0 + 16 * t) / 4;
+        load_words<NB>(k + (key * 16 + g * 4) * NB, kw[t]);
+        load_words<NB>(ke + (group + c / 4) * 4 * NB, kx[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        const uint32_t group = (key0 + 16 * t) / 4 + g;
+        load_words<NB>(v + (group * 64 + c * 4) * NB, vw[t]);
+        load_words<NB>(ve + group * 4 * NB, vx[t]);
+    }
+    float s[T][4];
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        const v4f x = scores16<NB, NP>(kw[t], kx[t], c & 3, q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s[t][i] = x[i] * scale2;
+            if (MASK) s[t][i] = key0 + 16 * t + 4 * g + i < limit ? s[t][i] : -INFINITY;
+            top = fmaxf(top, s[t][i]);
+        }
+    }
+    const float m_new = fmaxf(m, max_over_rows(top));
+    const float from = m_new == -INFINITY ? 0.0f : m_new;
+    if (__any(m_new > m)) {
+        const float shrink = __builtin_amdgcn_exp2f(m - from);
+        l *= shrink;
+#pragma unroll
+        for (int i = 0; i < 2 * NB; ++i) o[i] *= shrink;
+        m = m_new;
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s[t][i] = __builtin_amdgcn_exp2f(s[t][i] - from);
+            l += s[t][i];
+        }
+#pragma unroll
+    for (int u = 0; u < T; u += 2)
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) {
+            uint32_t w[4][NP];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    float x = s[u + t][i] * exponent_scale(vx[u + t][blk], i), y = s[u + t][i + 1] * exponent_scale(vx[u + t][blk], i + 1);
+                    if (MASK) {                             // a weight of 0 stays 0 whatever the exponent byte
+                        x = s[u + t][i] == 0.0f ? 0.0f : x;
+                        y = s[u + t][i + 1] == 0.0f ? 0.0f : y;
+                    }
+                    bf16_pieces2<NP>(x, y, w[2 * t + i / 2]);
+                }
+            const uint32_t lo0 = fp8_of_low(vw[u][blk]), lo1 = fp8_of_low(vw[u + 1][blk]);
+            const uint32_t hi0 = fp8_of_high(vw[u][blk]), hi1 = fp8_of_high(vw[u + 1][blk]);
+            const v4u lo = {bf16_pair<false>(lo0, 1.0f), bf16_pair<true>(lo0, 1.0f), bf16_pair<false>(lo1, 1.0f), bf16_pair<true>(lo1, 1.0f)};
+            const v4u hi = {bf16_pair<false>(hi0, 1.0f), bf16_pair<true>(hi0, 1.0f), bf16_pair<false>(hi1, 1.0f), bf16_pair<true>(hi1, 1.0f)};
+#pragma unroll
+            for (int p = NP - 1; p >= 0; --p) {
+                const v4u pw = {w[0][p], w[1][p], w[2][p], w[3][p]};
+                const v8bf pb = __builtin_bit_cast(v8bf, pw);
+                o[2 * blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, lo), pb, o[2 * blk], 0, 0, 0);
+                o[2 * blk + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, hi), pb, o[2 * blk + 1], 0, 0, 0);
+            }
+        }
+}
+
+// A workgroup's four waves take the steps of a chunk in turn and join their results in LDS; with several chunks the joined
+// ones go to the workspace, and cache_join_kernel joins those.
+template <int NB, int DT>
+__global__ __launch_bounds__(64 * kWaves, NB <= 4 ? 2 : 1) void cache_attend_kernel(const SplitParams p) {
+    constexpr int NP = Pieces<DT>::n, KS = NB <= 4 ? 64 : 32, DP = 32 * NB, PITCH = DP + 4;
+    extern __shared__ __attribute__((aligned(16))) float lds[];          // [wave][16 queries][PITCH], then [wave][16] max, [wave][16] sum
+    const CacheView &cache = p.a.c;
+    uint32_t id = blockIdx.x;
+    const int tile = (int)(id % p.tiles);
+    id /= p.tiles;
+    const uint32_t heads = cache.batch * cache.heads;
+    const int64_t bh = id % heads;
+    const int chunk = (int)(id / heads);
+    const int64_t b = bh / cache.heads;
+    const int key_head = (int)(bh % cache.heads);
+    const int length = p.a.lengths[b];
+    const int bound = p.a.longest;
+    const int last_row = 16 * tile + 15 < p.rows ? 16 * tile + 15 : p.rows - 1;
+    const int most = visible(length, p.a.tokens, p.a.group, last_row, p.a.causal, bound);
+    const int least = visible(length, p.a.tokens, p.a.group, 16 * tile, p.a.causal, bound);
+    const int begin = chunk * p.chunk, end = most < begin + p.chunk ? most : begin + p.chunk;
+    if (begin >= end && p.chunks > 1) return;                 // the whole workgroup, before any barrier
+
+    const int t = threadIdx.x, lane = t & 63, c = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int row = 16 * tile + c;
+    const int limit = row < p.rows ? visible(length, p.a.tokens, p.a.group, row, p.a.causal, bound) : 0;
+    v8bf q[NP][NB];
+    load_queries<NB, DT>(p.a.q, b, key_head, p.a.group, row, p.rows, cache.dim, g, q);
+    const uint8_t *k = cache.k + bh * cache.head_codes, *v = cache.v + bh * cache.head_codes;
+    const uint8_t *ke = cache.ke + bh * cache.head_exps, *ve = cache.ve + bh * cache.head_exps;
+    v4f o[2 * NB];
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i) o[i] = v4f{0, 0, 0, 0};
+    float m = -INFINITY, l = 0.0f;
+    for (int key0 = begin + wave * KS; key0 < end; key0 += kWaves * KS) {
+        if (key0 + KS <= least) attend_step<NB, NP, KS, false>(k, ke, v, ve, key0, limit, p.scale2, c, g, q, o, m, l);
+        else attend_step<NB, NP, KS, true>(k, ke, v, ve, key0, limit, p.scale2, c, g, q, o, m, l);
+    }
+    l = sum_over_rows(l);
+    float *const lds_m = lds + kWaves * 16 * PITCH, *const lds_l = lds_m + kWaves * 16;
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i) *reinterpret_cast<v4f *>(lds + (wave * 16 + c) * PITCH + 16 * i + 4 * g) = o[i];
+    if (g == 0) lds_m[wave * 16 + c] = m, lds_l[wave * 16 + c] = l;
+    __syncthreads();
+    const int rows_here = p.rows - 16 * tile < 16 ? p.rows - 16 * tile : 16;
+    for (int i = t; i < rows_here * (DP / 4); i += 64 * kWaves) {
+        const int r = i / (DP / 4), d = 4 * (i % (DP / 4));
+        float top = lds_m[r];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, lds_m[w * 16 + r]);
+        const float from = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f;
+        v4f acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float f = __builtin_amdgcn_exp2f(lds_m[w * 16 + r] - from);
+            sum += f * lds_l[w * 16 + r];
+            acc += f * *reinterpret_cast<const v4f *>(lds + (w * 16 + r) * PITCH + d);
+        }
+        const int grow = 16 * tile + r;
+        if (p.chunks > 1) {
+            const int64_t slot = (bh * p.chunks + chunk) * p.rows + grow;
+            *reinterpret_cast<v4f *>(p.o + slot * DP + d) = acc;
+            if (d == 0) p.ml[2 * slot] = top, p.ml[2 * slot + 1] = sum;
+        } else {
+            const int tok = grow / p.a.group, h = key_head * p.a.group + grow % p.a.group;
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const int64_t dst = b * p.a.out.sb + tok * p.a.out.st + h * p.a.out.sh + d;
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                if (d + x < cache.dim) store_float<DT>(p.a.out.data, dst + x, acc[x] * inv);
+            if (d == 0) p.a.lse[(b * p.a.tokens + tok) * p.a.heads + h] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+        }
+    }
+}
+
+// Joins the chunks of one row: sums in the chunks' order within each of the workgroup's parts, then over the parts.
+template <int DT>
+__global__ __launch_bounds__(256) void cache_join_kernel(const SplitParams p) {
+    __shared__ float lds[256 * 4 + 2 * 256];
+    const CacheView &cache = p.a.c;
+    const int row = (int)(blockIdx.x % p.rows);
+    const int64_t bh = blockIdx.x / p.rows;
+    const int64_t b = bh / cache.heads;
+    const int key_head = (int)(bh % cache.heads);
+    const int tile = row / 16, last_row = 16 * tile + 15 < p.rows ? 16 * tile + 15 : p.rows - 1;
+    const int most = visible(p.a.lengths[b], p.a.tokens, p.a.group, last_row, p.a.causal, p.a.longest);
+    const int n = (most + p.chunk - 1) / p.chunk;             // chunks that wrote
+    const int quads = 8 * cache.nblk, parts = 256 / quads;    // groups of four dimensions; at most 64
+    const int t = threadIdx.x, part = t / quads, d = 4 * (t % quads);
+    float m = -INFINITY, l = 0.0f;
+    v4f acc = {0, 0, 0, 0};
+    if (part < parts)
+        for (int i = part; i < n; i += parts) {
+            const int64_t slot = (bh * p.chunks + i) * p.rows + row;
+            const float mi = p.ml[2 * slot], li = p.ml[2 * slot + 1];
+            const v4f oi = *reinterpret_cast<const v4f *>(p.o + slot * 4 * quads + d);
+            const float top = fmaxf(m, mi), from = top == -INFINITY ? 0.0f : top;
+            const float f0 = __builtin_amdgcn_exp2f(m - from), f1 = __builtin_amdgcn_exp2f(mi - from);
+            l = l * f0 + li * f1;
+            acc = acc * f0 + oi * f1;
+            m = top;
+        }
+    float *const lds_m = lds + 1024, *const lds_l = lds_m + 256;
+    *reinterpret_cast<v4f *>(lds + 4 * t) = acc;
+    lds_m[t] = m;
+    lds_l[t] = l;
+    __syncthreads();
+    if (t >= quads) return;
+    float top = -INFINITY;
+    for (int i = 0; i < parts; ++i) top = fmaxf(top, lds_m[i * quads + t]);
+    const float from = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f;
+    acc = v4f{0, 0, 0, 0};
+    for (int i = 0; i < parts; ++i) {
+        const float f = __builtin_amdgcn_exp2f(lds_m[i * quads + t] - from);
+        sum += f * lds_l[i * quads + t];
+        acc += f * *reinterpret_cast<const v4f *>(lds + 4 * (i * quads + t));
+    }
+    const int tok = row / p.a.group, h = key_head * p.a.group + row % p.a.group;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int64_t dst = b * p.a.out.sb + tok * p.a.out.st + h * p.a.out.sh + d;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+        if (d + x < cache.dim) store_float<DT>(p.a.out.data, dst + x, acc[x] * inv);
+    if (t == 0) p.a.lse[(b * p.a.tokens + tok) * p.a.heads + h] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+// Chunks of keys: enough workgroups to fill the chip several times over, none shorter than a step of its four waves.
+SplitParams split_of(const AttendArgs &a) {
+    SplitParams p = {};
+    p.a = a;
+    p.rows = a.tokens * a.group;
+    p.tiles = (int32_t)ceil_div(p.rows, 16);
+    p.scale2 = a.scale * kLog2e;
+    const int64_t heads = (int64_t)a.c.batch * a.c.heads * p.tiles;
+    const int64_t step = kWaves * (a.c.nblk <= 4 ? 64 : 32);
+    const int64_t want = ceil_div(2048, heads);
+    p.chunk = (int32_t)round_up(ceil_div(a.longest, want), step);
+    p.chunks = (int32_t)ceil_div(a.longest, p.chunk);
+    return p;
+}
+size_t split_floats(const SplitParams &p) {
+    return p.chunks > 1 ? (size_t)p.a.c.batch * p.a.c.heads * p.chunks * p.rows * (size_t)(2 + 32 * p.a.c.nblk) : 0;
+}
+
+template <int NB, int DT>
+int launch_split(const SplitParams &p, hipStream_t s) {
+    static std::atomic<bool> configured;
+    constexpr int bytes = (kWaves * 16 * (32 * NB + 4) + 2 * kWaves * 16) * 4;
+    void (*const kernel)(SplitParams) = &cache_attend_kernel<NB, DT>;
+    if (allow_dynamic_lds(configured, reinterpret_cast<const void *>(kernel), bytes) != HBFP_OK) return HBFP_ERR_LAUNCH;
+    hipLaunchKernelGGL(kernel, dim3(p.wgs), dim3(64 * kWaves), bytes, s, p);
+    return launch_status();
+}
+template <int DT>
+int launch_split_of(const SplitParams &p, hipStream_t s) {
+    switch (p.a.c.nblk) {
+        case 1: return launch_split<1, DT>(p, s);
+        case 2: return launch_split<2, DT>(p, s);
+        case 3: return launch_split<3, DT>(p, s);
+        case 4: return launch_split<4, DT>(p, s);
+        case 5: return launch_split<5, DT>(p, s);
+        case 6: return launch_split<6, DT>(p, s);
+        case 7: return launch_split<7, DT>(p, s);
+        default: return launch_split<8, DT>(p, s);
+    }
+}
+
+// ---- accumulated weights.  A wave turns 64 keys into bf16 numbers once and meets every query of the key head with them; a
+// lane's sums over its query columns are exchanged over the 16 lanes at the end.
+struct WeighParams {
+    WeighArgs a;
+    int32_t rows, tiles;
+    float scale2;
+    int64_t units;               // batch * heads * groups of 64 slots
+};
+
+template <int NB, int DT>
+__global__ __launch_bounds__(256) void cache_weigh_kernel(const WeighParams p) {
+    constexpr int NP = Pieces<DT>::n;
+    const CacheView &cache = p.a.c;
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (unit >= p.units) return;
+    const int64_t heads = (int64_t)cache.batch * cache.heads, bh = unit % heads;
+    const int key0 = (int)(unit / heads) * 64;
+    const int64_t b = bh / cache.heads;
+    const int key_head = (int)(bh % cache.heads);
+    const int length = p.a.lengths[b], bound = cache.capacity;
+    const int held = visible(length, p.a.tokens, p.a.group, 0, 0, bound);
+    // this lane's result: value index c of its 16, key 16 (c / 4) + 4 g + c % 4
+    const int key = key0 + 16 * (c >> 2) + 4 * g + (c & 3);
+    const int64_t at = bh * p.a.ld + key;
+    if (key0 >= held) {
+        if (key < bound) p.a.w_out[at] = 0.0f;
+        return;
+    }
+    const float before = key < held ? p.a.w_in[at] : 0.0f;
+    const uint8_t *k = cache.k + bh * cache.head_codes, *ke = cache.ke + bh * cache.head_exps;
+    v8bf kf[4][NB];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        uint32_t w[NB], e[NB];
+        load_words<NB>(k + (uint32_t)((key0 + 16 * t + c) * 16 + g * 4) * NB, w);
+        load_words<NB>(ke + (uint32_t)((key0 + 16 * t) / 4 + c / 4) * 4 * NB, e);
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) kf[t][blk] = key_values(w[blk], exponent_scale(e[blk], c & 3));
+    }
+    float sum[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
+    for (int tile = 0; tile < p.tiles; ++tile) {
+        const int last_row = 16 * tile + 15 < p.rows ? 16 * tile + 15 : p.rows - 1;
+        if (visible(length, p.a.tokens, p.a.group, last_row, p.a.causal, bound) <= key0) continue;
+        const int row = 16 * tile + c;
+        int limit = 0;
+        float lse2 = 0.0f;
+        if (row < p.rows) {
+            limit = visible(length, p.a.tokens, p.a.group, row, p.a.causal, bound);
+            lse2 = p.a.lse[(b * p.a.tokens + row / p.a.group) * p.a.heads + key_head * p.a.group + row % p.a.group] * kLog2e;
+        }
+        v8bf q[NP][NB];
+        load_queries<NB, DT>(p.a.q, b, key_head, p.a.group, row, p.rows, cache.dim, g, q);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            v4f s = {0, 0, 0, 0};
+#pragma unroll
+            for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+                for (int i = NP - 1; i >= 0; --i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][blk], q[i][blk], s, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x = __builtin_amdgcn_exp2f(s[i] * p.scale2 - lse2);
+                sum[4 * t + i] += key0 + 16 * t + 4 * g + i < limit ? x : 0.0f;
+            }
+        }
+    }
+    // over the 16 lanes of a row: each exchange halves the values a lane carries
+#pragma unroll
+    for (int half = 8; half >= 1; half >>= 1) {
+        const bool upper = (c & half) != 0;
+#pragma unroll
+        for (int i = 0; i < half; ++i) {
+            const float keep = upper ? sum[i + half] : sum[i], give = upper ? sum[i] : sum[i + half];
+            sum[i] = keep + __shfl_xor(give, half);
+        }
+    }
+    if (key < bound) p.a.w_out[at] = key < held ? p.a.decay * before + sum[0] : 0.0f;
+}
+
+template <int DT>
+int launch_weigh_of(const WeighParams &p, hipStream_t s) {
+    static void (*const kernels[8])(WeighParams) = {&cache_weigh_kernel<1, DT>, &cache_weigh_kernel<2, DT>, &cache_weigh_kernel<3, DT>,
+                                                    &cache_weigh_kernel<4, DT>, &cache_weigh_kernel<5, DT>, &cache_weigh_kernel<6, DT>,
+                                                    &cache_weigh_kernel<7, DT>, &cache_weigh_kernel<8, DT>};
+    const int64_t wgs = ceil_div(p.units, 4);
+    if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
+    hipLaunchKernelGGL(kernels[p.a.c.nblk - 1], dim3((unsigned)wgs), dim3(256), 0, s, p);
+    return launch_status();
+}
+
+}  // namespace
+
+size_t cache_attend_workspace(const AttendArgs &a, int dtype) {
+    (void)dtype;
+    return split_floats(split_of(a)) * 4;
+}
+
+int launch_cache_attend(const AttendArgs &a, int dtype, hipStream_t s) {
+    SplitParams p = split_of(a);
+    const int64_t heads = (int64_t)a.c.batch * a.c.heads;
+    const int64_t wgs = heads * p.tiles * p.chunks, rows = heads * p.rows;
+    if (wgs > 0x7fffffff || rows > 0x7fffffff) return HBFP_ERR_ARG;
+    p.wgs = (uint32_t)wgs;
+    p.o = a.ws;
+    p.ml = a.ws ? a.ws + heads * p.chunks * p.rows * 32 * a.c.nblk : nullptr;
+    int rc = dtype == HBFP_F32 ? launch_split_of<HBFP_F32>(p, s) : dtype == HBFP_BF16 ? launch_split_of<HBFP_BF16>(p, s) : launch_split_of<HBFP_F16>(p, s);
+    if (rc != HBFP_OK || p.chunks == 1) return rc;
+    void (*const join)(SplitParams) = dtype == HBFP_F32    ? &cache_join_kernel<HBFP_F32>
+                                      : dtype == HBFP_BF16 ? &cache_join_kernel<HBFP_BF16>
+                                                           : &cache_join_kernel<HBFP_F16>;
+    hipLaunchKernelGGL(join, dim3((unsigned)rows), dim3(256), 0, s, p);
+    return launch_status();
+}
+
+int launch_cache_weigh(const WeighArgs &a, int dtype, hipStream_t s) {
+    WeighParams p = {};
+    p.a = a;
+    p.rows = a.tokens * a.group;
+    p.tiles = (int32_t)ceil_div(p.rows, 16);
+    p.scale2 = a.scale * kLog2e;
+    p.units = (int64_t)a.c.batch * a.c.heads * ceil_div(a.c.capacity, 64);
+    return dtype == HBFP_F32 ? launch_weigh_of<HBFP_F32>(p, s) : dtype == HBFP_BF16 ? launch_weigh_of<HBFP_BF16>(p, s) : launch_weigh_of<HBFP_F16>(p, s);
+}
+
+}  // namespace hbfp

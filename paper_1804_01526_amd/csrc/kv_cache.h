@@ -1,0 +1,113 @@
+// Device side of the 4-bit cache: its layout (stated in the public header), the way from nibbles to bf16 and loads and
+// stores of the three tensor types.
+#pragma once
+#include "hbfp_internal.h"
+#include "serve.h"
+
+namespace hbfp {
+namespace {
+
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
+// ---- nibbles -> numbers.  A nibble is sign and magnitude, so that one byte permute looks four magnitudes up in a table of
+// eight FP8 (E4M3) numbers, n / 4, and the sign is the fourth bit moved to the eighth: four instructions for the four low or
+// the four high nibbles of a word.  The conversion FP8 -> bf16 multiplies by a power of two, whose FP32 exponent field is
+// the block's exponent byte itself: n / 4 * 2^(Eb - 127) = n * 2^(Eb - 129).  Exact for every Eb up to 254, subnormal results
+// included; Eb = 255 gives NaN.
+__device__ __forceinline__ uint32_t fp8_of_low(uint32_t w) {
+    return __builtin_amdgcn_perm(0x3E3C3A38u, 0x34302800u, w & 0x07070707u) | ((w << 4) & 0x80808080u);
+}
+__device__ __forceinline__ uint32_t fp8_of_high(uint32_t w) {
+    return __builtin_amdgcn_perm(0x3E3C3A38u, 0x34302800u, (w >> 4) & 0x07070707u) | (w & 0x80808080u);
+}
+// bytes 0 and 1 (HIGH: 2 and 3) as two bf16 numbers times scale, a power of two
+template <bool HIGH>
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t fp8, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(fp8, scale, HIGH));
+}
+// the 2^(Eb - 127) of the exponent byte `j` of a word
+__device__ __forceinline__ float exponent_scale(uint32_t word, int j) { return __uint_as_float(((word >> (8 * j)) & 0xffu) << 23); }
+
+// eight values in the order low nibbles, high nibbles (for the key layout: dimensions 8 g .. 8 g + 7)
+__device__ __forceinline__ v8bf key_values(uint32_t w, float scale) {
+    const uint32_t lo = fp8_of_low(w), hi = fp8_of_high(w);
+    const v4u r = {bf16_pair<false>(lo, scale), bf16_pair<true>(lo, scale), bf16_pair<false>(hi, scale), bf16_pair<true>(hi, scale)};
+    return __builtin_bit_cast(v8bf, r);
+}
+
+// ---- the three tensor types
+template <int DT>
+__device__ __forceinline__ float load_as_float(const void *p, int64_t i) {
+    if (DT == HBFP_F32) return reinterpret_cast<const float *>(p)[i];
+    if (DT == HBFP_BF16) return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << 16);
+    return (float)reinterpret_cast<const _Float16 *>(p)[i];
+}
+template <int DT>
+__device__ __forceinline__ void store_float(void *p, int64_t i, float x) {
+    if (DT == HBFP_F32) reinterpret_cast<float *>(p)[i] = x;
+    else if (DT == HBFP_BF16) reinterpret_cast<__bf16 *>(p)[i] = (__bf16)x;
+    else reinterpret_cast<_Float16 *>(p)[i] = (_Float16)x;
+}
+// eight consecutive elements from i on, of which n (may be <= 0) exist, the others 0; whole: all exist and the address allows wide loads
+template <int DT>
+__device__ __forceinline__ void load8(const void *p, int64_t i, int n, bool whole, float *x) {
+    if (whole) {
+        if (DT == HBFP_F32) {
+            const v4f a = *reinterpret_cast<const v4f *>(reinterpret_cast<const float *>(p) + i);
+            const v4f b = *reinterpret_cast<const v4f *>(reinterpret_cast<const float *>(p) + i + 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = a[j], x[4 + j] = b[j];
+        } else {
+            const v4u a = *reinterpret_cast<const v4u *>(reinterpret_cast<const uint16_t *>(p) + i);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t h = j & 1 ? a[j / 2] >> 16 : a[j / 2] & 0xffffu;
+                x[j] = DT == HBFP_BF16 ? __uint_as_float(h << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)h);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = j < n ? load_as_float<DT>(p, i + j) : 0.0f;
+}
+
+__device__ __forceinline__ uint32_t bf16_bits2(float a, float b) {
+    const v2bf r = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, r);
+}
+// x as a sum of N bf16 numbers, the first N * 8 bits of it: piece p of two values
+template <int N>
+__device__ __forceinline__ void bf16_pieces2(float a, float b, uint32_t *out) {
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+        out[p] = bf16_bits2(a, b);
+        a -= __uint_as_float(out[p] << 16);
+        b -= __uint_as_float(out[p] & 0xffff0000u);
+    }
+}
+
+// bf16 numbers a type's values (and softmax weights of its calls) are cut into: bf16 8 bits, FP16 11 bits, FP32 24 bits
+template <int DT> struct Pieces { static constexpr int n = DT == HBFP_F32 ? 3 : DT == HBFP_F16 ? 2 : 1; };
+
+// largest of the lanes l, l ^ 16, l ^ 32, l ^ 48, and the sum: two exchanges of rows of lanes on the vector unit
+__device__ __forceinline__ float max_over_rows(float x) {
+    const v2u a = __builtin_bit_cast(v2u, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const v2u b = __builtin_bit_cast(v2u, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_over_rows(float x) {
+    const v2u a = __builtin_bit_cast(v2u, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const v2u b = __builtin_bit_cast(v2u, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+}  // namespace
+}  // namespace hbfp

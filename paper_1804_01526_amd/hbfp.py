@@ -63,6 +63,19 @@ class TensorDesc(ctypes.Structure):
                 ("seed", ctypes.c_uint64), ("mant_bytes", ctypes.c_uint64), ("exp_bytes", ctypes.c_uint64)]
 
 
+class CacheDesc(ctypes.Structure):
+    """hbfp_cache: keys and values in 4-bit BFP (layout in include/hbfp.h)."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exps", ctypes.c_void_p), ("v_exps", ctypes.c_void_p),
+                ("batch", ctypes.c_int64), ("heads", ctypes.c_int64), ("capacity", ctypes.c_int64), ("dim", ctypes.c_int64),
+                ("slots", ctypes.c_int64), ("nblk", ctypes.c_int64), ("code_bytes", ctypes.c_uint64), ("exp_bytes", ctypes.c_uint64)]
+
+
+class Heads(ctypes.Structure):
+    """hbfp_heads: one call's tensor [batch][tokens][heads][dim]."""
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("stride_batch", ctypes.c_int64), ("stride_token", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
+
+
 def _load():
     if not os.path.exists(_LIB_PATH):
         raise ImportError(
@@ -128,6 +141,24 @@ def _load():
     lib.hbfp_probe_matrix_rate.restype = i32
     lib.hbfp_weight_update_workspace.argtypes = [T, T, T, ctypes.POINTER(sz)]
     lib.hbfp_weight_update.argtypes = [T, vp, i64, ctypes.c_float, T, T, vp, sz, vp]
+    KV, H, f32 = ctypes.POINTER(CacheDesc), ctypes.POINTER(Heads), ctypes.c_float
+    lib.hbfp_cache_plan.argtypes = [i64, i64, i64, i64, KV]
+    lib.hbfp_cache_append.argtypes = [KV, H, H, i64, vp, vp, vp, vp]
+    lib.hbfp_cache_read.argtypes = [KV, vp, i32, vp, vp, vp]
+    lib.hbfp_cache_attend_workspace.argtypes = [KV, i64, i64, i32, i64, ctypes.POINTER(sz)]
+    lib.hbfp_cache_attend.argtypes = [KV, H, i64, i64, vp, i64, f32, i32, H, vp, vp, sz, vp]
+    lib.hbfp_cache_weigh.argtypes = [KV, H, i64, i64, vp, f32, i32, vp, f32, vp, vp, i64, vp]
+    lib.hbfp_cache_evict.argtypes = [KV, vp, i64, vp, i64, i64, KV, vp, i64, vp, vp, vp]
+    lib.hbfp_rows_plan.argtypes = [i64, i64, ctypes.POINTER(i64), ctypes.POINTER(sz)]
+    lib.hbfp_quant_rows.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
+    lib.hbfp_gemm_rows_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(sz)]
+    lib.hbfp_gemm_rows.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, i32, i64, vp, sz, vp]
+    lib.hbfp_linear_i8_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(sz)]
+    lib.hbfp_linear_i8.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, i64, vp, i64, vp, sz, vp]
+    for name in ("hbfp_cache_plan", "hbfp_cache_append", "hbfp_cache_read", "hbfp_cache_attend_workspace", "hbfp_cache_attend",
+                 "hbfp_cache_weigh", "hbfp_cache_evict", "hbfp_rows_plan", "hbfp_quant_rows", "hbfp_gemm_rows_workspace",
+                 "hbfp_gemm_rows", "hbfp_linear_i8_workspace", "hbfp_linear_i8"):
+        getattr(lib, name).restype = i32
     for name in ("hbfp_gemm_batch_workspace", "hbfp_gemm_batch", "hbfp_gemm_bfp_workspace", "hbfp_gemm_bfp", "hbfp_encode_im2col", "hbfp_encode_multi_workspace", "hbfp_encode_multi", "hbfp_encode_packed_workspace", "hbfp_encode_packed", "hbfp_encode_packed_batch_workspace", "hbfp_encode_packed_batch", "hbfp_weight_update_workspace", "hbfp_weight_update", "hbfp_plan", "hbfp_encode_workspace", "hbfp_encode", "hbfp_encode_static", "hbfp_decode", "hbfp_gemm_workspace",
                  "hbfp_gemm", "hbfp_gemm_select_workspace", "hbfp_gemm_select", "hbfp_pack_bytes", "hbfp_pack",
                  "hbfp_gemm_packed_workspace", "hbfp_gemm_packed", "hbfp_gemm_packed_batch_workspace", "hbfp_gemm_packed_batch", "hbfp_gemm_partials", "hbfp_gemm_partials_window", "hbfp_gemm_f32_workspace",
@@ -640,4 +671,221 @@ def gemm_conv2d_dgrad(dy: BfpTensor, conv: Conv2d, filters: BfpTensor, out: Opti
     _check(_lib.hbfp_gemm_conv2d_dgrad(ctypes.byref(dy.desc), ctypes.byref(conv), ctypes.byref(filters.desc), _dev_ptr(out),
                                        out.stride(0), beta, _dev_ptr(workspace), 0 if workspace is None else workspace.numel(),
                                        _stream_ptr(stream)), "hbfp_gemm_conv2d_dgrad")
+    return out
+
+
+# ---------------------------------------------------------------------------- serving: the 4-bit cache
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _buffer(shape, dtype, device, stream) -> torch.Tensor:
+    """A tensor that a call on `stream` writes: the allocator must not hand its memory on before that stream is done with it."""
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None and t.numel():
+        t.record_stream(stream)
+    return t
+
+
+def _heads(t: torch.Tensor, batch: int, tokens: int, heads: int, dim: int, device) -> Heads:
+    assert t.device == device and t.dtype in _TYPES, "a tensor of FP32, bf16 or FP16 on the cache's GPU"
+    assert tuple(t.shape) == (batch, tokens, heads, dim), f"shape {tuple(t.shape)}, expected {(batch, tokens, heads, dim)}"
+    assert dim == 1 or t.stride(3) == 1, "the head dimension must be contiguous"
+    st = [0 if t.shape[i] == 1 else t.stride(i) for i in range(3)]
+    return Heads(t.data_ptr(), _TYPES[t.dtype], 0, *st)
+
+
+def _lengths(lengths: torch.Tensor, batch: int, device):
+    assert lengths.device == device and lengths.dtype == torch.int32 and lengths.is_contiguous() and lengths.numel() == batch
+    return _dev_ptr(lengths)
+
+
+@dataclass
+class KvCache:
+    """Keys and values of one layer in 4-bit BFP: the descriptor plus the torch buffers behind its four pointers."""
+    desc: CacheDesc
+    k: torch.Tensor        # uint8 [batch, heads, slots * 16 * nblk]
+    v: torch.Tensor
+    k_exps: torch.Tensor   # uint8 [batch, heads, slots * nblk]
+    v_exps: torch.Tensor
+
+
+def _cache(desc: CacheDesc, k, v, k_exps, v_exps) -> KvCache:
+    desc.k, desc.v, desc.k_exps, desc.v_exps = (t.data_ptr() for t in (k, v, k_exps, v_exps))
+    return KvCache(desc, k, v, k_exps, v_exps)
+
+
+def cache_plan(batch: int, heads: int, capacity: int, dim: int) -> CacheDesc:
+    d = CacheDesc()
+    _check(_lib.hbfp_cache_plan(batch, heads, capacity, dim, ctypes.byref(d)), "hbfp_cache_plan")
+    return d
+
+
+def cache_alloc(batch: int, heads: int, capacity: int, dim: int, device="cuda") -> KvCache:
+    """An empty cache for `capacity` tokens of each batch entry (its contents are whatever the memory holds)."""
+    d = cache_plan(batch, heads, capacity, dim)
+    codes = [torch.empty((batch, heads, d.slots * 16 * d.nblk), dtype=torch.uint8, device=device) for _ in range(2)]
+    exps = [torch.empty((batch, heads, d.slots * d.nblk), dtype=torch.uint8, device=device) for _ in range(2)]
+    return _cache(d, *codes, *exps)
+
+
+def cache_rows(cache: KvCache, first: int, last: int) -> KvCache:
+    """The batch entries first .. last - 1 of a cache, as a cache over the same memory."""
+    assert 0 <= first < last <= cache.desc.batch
+    d = cache_plan(last - first, cache.desc.heads, cache.desc.capacity, cache.desc.dim)
+    return _cache(d, *(t[first:last] for t in (cache.k, cache.v, cache.k_exps, cache.v_exps)))
+
+
+def cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, lengths: torch.Tensor, values: bool = False, stream=None):
+    """hbfp_cache_append: k, v [batch, tokens, heads, dim]; lengths (int32, on the GPU) count the new tokens.  values: returns the
+    values that the cache now holds for them, a pair of bf16 tensors of k's shape."""
+    d, tokens = cache.desc, k.shape[1]
+    hk, hv = (_heads(t, d.batch, tokens, d.heads, d.dim, cache.k.device) for t in (k, v))
+    held = tuple(_buffer(k.shape, torch.bfloat16, k.device, stream) for _ in range(2)) if values else (None, None)
+    _check(_lib.hbfp_cache_append(ctypes.byref(d), ctypes.byref(hk), ctypes.byref(hv), tokens, _lengths(lengths, d.batch, cache.k.device),
+                                  _dev_ptr(held[0]), _dev_ptr(held[1]), _stream_ptr(stream)), "hbfp_cache_append")
+    return held if values else None
+
+
+def cache_read(cache: KvCache, lengths: torch.Tensor, dtype=torch.float32, stream=None):
+    """hbfp_cache_read: (keys, values) [batch, heads, capacity, dim], 0 from each length on."""
+    d = cache.desc
+    assert dtype in _TYPES
+    k, v = (_buffer((d.batch, d.heads, d.capacity, d.dim), dtype, cache.k.device, stream) for _ in range(2))
+    _check(_lib.hbfp_cache_read(ctypes.byref(d), _lengths(lengths, d.batch, cache.k.device), _TYPES[dtype], _dev_ptr(k), _dev_ptr(v),
+                                _stream_ptr(stream)), "hbfp_cache_read")
+    return k, v
+
+
+def cache_attend_workspace(desc: CacheDesc, tokens: int, heads: int, dtype=torch.bfloat16, longest: int = 0) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.hbfp_cache_attend_workspace(ctypes.byref(desc), tokens, heads, _TYPES[dtype], longest, ctypes.byref(n)),
+           "hbfp_cache_attend_workspace")
+    return int(n.value)
+
+
+def cache_attend(cache: KvCache, q: torch.Tensor, lengths: torch.Tensor, scale: Optional[float] = None, causal: bool = True,
+                 longest: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None, stream=None):
+    """hbfp_cache_attend: (out, lse) for q [batch, tokens, query heads, dim]; scale defaults to dim ** -0.5."""
+    d = cache.desc
+    tokens, heads = q.shape[1], q.shape[2]
+    hq = _heads(q, d.batch, tokens, heads, d.dim, cache.k.device)
+    if out is None:
+        out = _buffer(q.shape, q.dtype, q.device, stream)
+    if lse is None:
+        lse = _buffer((d.batch, tokens, heads), torch.float32, q.device, stream)
+    assert lse.device == q.device and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:3]
+    ho = _heads(out, d.batch, tokens, heads, d.dim, cache.k.device)
+    if workspace is None:
+        need = cache_attend_workspace(d, tokens, heads, q.dtype, longest)
+        workspace = _buffer((need,), torch.uint8, q.device, stream) if need else None
+    _check(_lib.hbfp_cache_attend(ctypes.byref(d), ctypes.byref(hq), tokens, heads, _lengths(lengths, d.batch, q.device), longest,
+                                  d.dim ** -0.5 if scale is None else scale, 1 if causal else 0, ctypes.byref(ho), _dev_ptr(lse),
+                                  _dev_ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream)),
+           "hbfp_cache_attend")
+    return out, lse
+
+
+def cache_weigh(cache: KvCache, q: torch.Tensor, lse: torch.Tensor, lengths: torch.Tensor, weights: torch.Tensor,
+                scale: Optional[float] = None, causal: bool = True, decay: float = 1.0, out: Optional[torch.Tensor] = None,
+                stream=None) -> torch.Tensor:
+    """hbfp_cache_weigh: out = decay * weights + the attention weight each cached token received; weights FP32 [batch, heads, n],
+    n >= capacity; out defaults to weights (in place)."""
+    d = cache.desc
+    tokens, heads = q.shape[1], q.shape[2]
+    hq = _heads(q, d.batch, tokens, heads, d.dim, cache.k.device)
+    out = weights if out is None else out
+    for t in (weights, out):
+        assert t.device == q.device and t.dtype == torch.float32 and t.is_contiguous() and t.dim() == 3
+        assert t.shape[:2] == (d.batch, d.heads) and t.shape == weights.shape
+    assert lse.device == q.device and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:3]
+    _check(_lib.hbfp_cache_weigh(ctypes.byref(d), ctypes.byref(hq), tokens, heads, _lengths(lengths, d.batch, q.device),
+                                 d.dim ** -0.5 if scale is None else scale, 1 if causal else 0, _dev_ptr(lse), decay, _dev_ptr(weights),
+                                 _dev_ptr(out), weights.shape[2], _stream_ptr(stream)), "hbfp_cache_weigh")
+    return out
+
+
+def cache_evict(cache: KvCache, weights: torch.Tensor, lengths: torch.Tensor, out: KvCache, keep: int, recent: int,
+                out_weights: Optional[torch.Tensor] = None, stream=None):
+    """hbfp_cache_evict into the cache `out`: (kept slots [batch, heads, keep], new lengths, their weights [batch, heads, n])."""
+    d, device = cache.desc, cache.k.device
+    assert weights.device == device and weights.dtype == torch.float32 and weights.is_contiguous() and weights.dim() == 3
+    assert weights.shape[:2] == (d.batch, d.heads) and out.k.device == device
+    if out_weights is None:
+        out_weights = _buffer((d.batch, d.heads, out.desc.capacity), torch.float32, device, stream)
+    assert out_weights.device == device and out_weights.dtype == torch.float32 and out_weights.is_contiguous() and out_weights.dim() == 3
+    assert out_weights.shape[:2] == (d.batch, d.heads)
+    kept = _buffer((d.batch, d.heads, max(keep, 1)), torch.int32, device, stream)
+    new_lengths = _buffer((d.batch,), torch.int32, device, stream)
+    _check(_lib.hbfp_cache_evict(ctypes.byref(d), _dev_ptr(weights), weights.shape[2], _lengths(lengths, d.batch, device), keep, recent,
+                                 ctypes.byref(out.desc), _dev_ptr(out_weights), out_weights.shape[2], _dev_ptr(kept),
+                                 _dev_ptr(new_lengths), _stream_ptr(stream)), "hbfp_cache_evict")
+    return kept, new_lengths, out_weights
+
+
+# ---------------------------------------------------------------------------- serving: products with a scale per row
+@dataclass
+class RowCodes:
+    """A matrix as rows of 8-bit codes with one FP32 scale each."""
+    codes: torch.Tensor    # int8 [rows, kpad], 0 from cols on
+    scales: torch.Tensor   # FP32 [rows]
+    cols: int
+
+
+def _matrix(t: torch.Tensor):
+    assert t.is_cuda and t.dtype in _TYPES and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "FP32, bf16 or FP16 rows"
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def quant_rows(x: torch.Tensor, stream=None) -> RowCodes:
+    """hbfp_quant_rows of x [rows, cols]: a linear layer's weights [out features, in features], once; or tokens."""
+    ld = _matrix(x)
+    kpad = ctypes.c_int64(0)
+    _check(_lib.hbfp_rows_plan(x.shape[0], x.shape[1], ctypes.byref(kpad), None), "hbfp_rows_plan")
+    codes = _buffer((x.shape[0], kpad.value), torch.int8, x.device, stream)
+    scales = _buffer((x.shape[0],), torch.float32, x.device, stream)
+    _check(_lib.hbfp_quant_rows(_dev_ptr(x), _TYPES[x.dtype], x.shape[0], x.shape[1], ld, _dev_ptr(codes), _dev_ptr(scales),
+                                _stream_ptr(stream)), "hbfp_quant_rows")
+    return RowCodes(codes, scales, x.shape[1])
+
+
+def _product_out(bias, w: RowCodes, rows: int, dtype, device, out, stream):
+    n = w.codes.shape[0]
+    assert w.codes.device == device
+    if bias is not None:
+        assert bias.device == device and bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == n
+    if out is None:
+        out = _buffer((rows, n), dtype, device, stream)
+    assert out.device == device and out.dtype == dtype and tuple(out.shape) == (rows, n)
+    return out, _matrix(out)
+
+
+def gemm_rows(a: RowCodes, w: RowCodes, bias: Optional[torch.Tensor] = None, dtype=torch.float32, out: Optional[torch.Tensor] = None,
+              workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """hbfp_gemm_rows: y [rows of a, rows of w] = a . w^T (+ bias), rounded once to `dtype`."""
+    assert a.cols == w.cols
+    m, n, device = a.codes.shape[0], w.codes.shape[0], a.codes.device
+    out, ld = _product_out(bias, w, m, dtype if out is None else out.dtype, device, out, stream)
+    if workspace is None:
+        need = ctypes.c_size_t(0)
+        _check(_lib.hbfp_gemm_rows_workspace(m, n, a.cols, ctypes.byref(need)), "hbfp_gemm_rows_workspace")
+        workspace = _buffer((need.value,), torch.uint8, device, stream) if need.value else None
+    _check(_lib.hbfp_gemm_rows(_dev_ptr(a.codes), _dev_ptr(a.scales), _dev_ptr(w.codes), _dev_ptr(w.scales), _dev_ptr(bias), m, n, a.cols,
+                               _dev_ptr(out), _TYPES[out.dtype], ld, _dev_ptr(workspace), 0 if workspace is None else workspace.numel(),
+                               _stream_ptr(stream)), "hbfp_gemm_rows")
+    return out
+
+
+def linear_i8(x: torch.Tensor, w: RowCodes, bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+              workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """hbfp_linear_i8: y = quant(x) . w^T (+ bias) in x's type, for x [tokens, in features] and weights from quant_rows."""
+    ldx, (m, k), n = _matrix(x), x.shape, w.codes.shape[0]
+    assert k == w.cols
+    out, ldy = _product_out(bias, w, m, x.dtype, x.device, out, stream)
+    if workspace is None:
+        need = ctypes.c_size_t(0)
+        _check(_lib.hbfp_linear_i8_workspace(m, n, k, ctypes.byref(need)), "hbfp_linear_i8_workspace")
+        workspace = _buffer((need.value,), torch.uint8, x.device, stream)
+    _check(_lib.hbfp_linear_i8(_dev_ptr(x), _TYPES[x.dtype], m, k, ldx, _dev_ptr(w.codes), _dev_ptr(w.scales), _dev_ptr(bias), n,
+                               _dev_ptr(out), ldy, _dev_ptr(workspace), workspace.numel(), _stream_ptr(stream)), "hbfp_linear_i8")
     return out
