@@ -1,12 +1,11 @@
 // Products in 8-bit integers with an FP32 scale per row of each operand:
 //     y[m][n] = (sum_k a[m][k] b[n][k]) * sa[m] * sb[n] + bias[n]
 // The sum is an exact int32 whatever its order; scales and bias are FP32 and y is rounded once.
+#include "gemm_wide.h"
 #include "kv_cache.h"
 
 namespace hbfp {
 namespace {
-
-typedef int v4i __attribute__((ext_vector_type(4)));
 
 // ---- rows -> codes.  A workgroup has one row; it reads the row twice, the second time from the caches.
 struct QuantParams {
@@ -110,8 +109,7 @@ __global__ __launch_bounds__(256) void gemm_rows_few_kernel(const FewParams p) {
         for (int v = 0; v < 4; ++v) {
             const int64_t n = n0 + 4 * g + v;
             if (n >= r.N) continue;
-            const float y = (float)all[v] * sa * r.sb[n];
-            store_float<DT>(r.y, m * r.ldy + n, r.bias ? y + r.bias[n] : y);
+            store_float<DT>(r.y, m * r.ldy + n, scaled_sum(all[v], sa, r.sb[n], r.bias ? r.bias[n] : 0.0f, r.bias != nullptr));
         }
     }
 }
@@ -140,14 +138,40 @@ int launch_quant_rows(const void *src, int dtype, int64_t rows, int64_t cols, in
     return launch_status();
 }
 
+// Few tokens are a pass over b, the others tiles on the matrix core.
+static bool few_rows(int64_t M) { return M <= 64; }
+
 size_t gemm_rows_workspace(int64_t M, int64_t N, int64_t kpad) {
-    (void)M, (void)N, (void)kpad;
-    return 0;
+    if (few_rows(M)) return 0;
+    const WidePlan plan = wide_plan(M, N, kpad / 64, true);
+    return plan.splits > 1 ? (size_t)plan.splits * (size_t)M * (size_t)N * 4 : 0;
 }
 
 int launch_gemm_rows(const RowsArgs &a, void *workspace, hipStream_t s) {
-    (void)workspace;
-    return a.dtype == HBFP_F32 ? launch_few<HBFP_F32>(a, s) : a.dtype == HBFP_BF16 ? launch_few<HBFP_BF16>(a, s) : launch_few<HBFP_F16>(a, s);
+    if (few_rows(a.M)) return a.dtype == HBFP_F32 ? launch_few<HBFP_F32>(a, s) : a.dtype == HBFP_BF16 ? launch_few<HBFP_BF16>(a, s) : launch_few<HBFP_F16>(a, s);
+    if (ceil_div(a.M, 128) * ceil_div(a.N, 128) > 0x7ffffff0) return HBFP_ERR_ARG;
+    const WidePlan plan = wide_plan(a.M, a.N, a.kpad / 64, true);
+    WideParams p = {};
+    p.A = (const uint8_t *)a.a;
+    p.B = (const uint8_t *)a.b;
+    p.C = (float *)a.y;
+    p.partial = (int32_t *)workspace;
+    p.M = a.M;
+    p.N = a.N;
+    p.kpad = a.kpad;
+    p.ldc = a.ldy;
+    p.sa = a.sa;
+    p.sb = a.sb;
+    p.bias = a.bias;
+    GemmArgs g = {};
+    g.M = a.M;
+    g.N = a.N;
+    g.C = (float *)a.y;
+    g.ldc = a.ldy;
+    const bool stream = a.kpad > 1024 || stores_stream(&g);
+    return a.dtype == HBFP_F32    ? launch_wide_planned<kWideF32>(p, plan, stream, s)
+           : a.dtype == HBFP_BF16 ? launch_wide_planned<kWideBf16>(p, plan, stream, s)
+                                  : launch_wide_planned<kWideF16>(p, plan, stream, s);
 }
 
 }  // namespace hbfp

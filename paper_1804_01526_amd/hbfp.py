@@ -7,6 +7,7 @@ library has not been built, importing this module fails.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -687,16 +688,26 @@ def _buffer(shape, dtype, device, stream) -> torch.Tensor:
 
 
 def _heads(t: torch.Tensor, batch: int, tokens: int, heads: int, dim: int, device) -> Heads:
-    assert t.device == device and t.dtype in _TYPES, "a tensor of FP32, bf16 or FP16 on the cache's GPU"
-    assert tuple(t.shape) == (batch, tokens, heads, dim), f"shape {tuple(t.shape)}, expected {(batch, tokens, heads, dim)}"
-    assert dim == 1 or t.stride(3) == 1, "the head dimension must be contiguous"
-    st = [0 if t.shape[i] == 1 else t.stride(i) for i in range(3)]
-    return Heads(t.data_ptr(), _TYPES[t.dtype], 0, *st)
+    assert t.dtype in _TYPES and t.device == device, "a tensor of FP32, bf16 or FP16 on the cache's GPU"
+    assert t.shape == (batch, tokens, heads, dim), f"shape {tuple(t.shape)}, expected {(batch, tokens, heads, dim)}"
+    sb, st, sh, sd = t.stride()
+    assert sd == 1 or dim == 1, "the head dimension must be contiguous"
+    return Heads(t.data_ptr(), _TYPES[t.dtype], 0, sb if batch > 1 else 0, st if tokens > 1 else 0, sh if heads > 1 else 0)
 
 
-def _lengths(lengths: torch.Tensor, batch: int, device):
-    assert lengths.device == device and lengths.dtype == torch.int32 and lengths.is_contiguous() and lengths.numel() == batch
-    return _dev_ptr(lengths)
+def _lengths(lengths: torch.Tensor, batch: int, device) -> int:
+    assert lengths.dtype == torch.int32 and lengths.device == device and lengths.is_contiguous() and lengths.numel() == batch
+    return lengths.data_ptr()
+
+
+def _raw_stream(stream, device) -> int:
+    """The stream a call goes to.  A decode step is a few microseconds of kernels, and a torch.cuda.Stream object for each of its calls
+    costs one of them; this is the handle alone."""
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
 
 
 @dataclass
@@ -738,28 +749,33 @@ def cache_rows(cache: KvCache, first: int, last: int) -> KvCache:
 def cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, lengths: torch.Tensor, values: bool = False, stream=None):
     """hbfp_cache_append: k, v [batch, tokens, heads, dim]; lengths (int32, on the GPU) count the new tokens.  values: returns the
     values that the cache now holds for them, a pair of bf16 tensors of k's shape."""
-    d, tokens = cache.desc, k.shape[1]
-    hk, hv = (_heads(t, d.batch, tokens, d.heads, d.dim, cache.k.device) for t in (k, v))
-    held = tuple(_buffer(k.shape, torch.bfloat16, k.device, stream) for _ in range(2)) if values else (None, None)
-    _check(_lib.hbfp_cache_append(ctypes.byref(d), ctypes.byref(hk), ctypes.byref(hv), tokens, _lengths(lengths, d.batch, cache.k.device),
-                                  _dev_ptr(held[0]), _dev_ptr(held[1]), _stream_ptr(stream)), "hbfp_cache_append")
+    d, tokens, device = cache.desc, k.shape[1], cache.k.device
+    batch, heads, dim = d.batch, d.heads, d.dim
+    hk, hv = _heads(k, batch, tokens, heads, dim, device), _heads(v, batch, tokens, heads, dim, device)
+    held = tuple(_buffer(k.shape, torch.bfloat16, device, stream) for _ in range(2)) if values else (None, None)
+    _check(_lib.hbfp_cache_append(ctypes.byref(d), ctypes.byref(hk), ctypes.byref(hv), tokens, _lengths(lengths, batch, device),
+                                  _ptr(held[0]), _ptr(held[1]), _raw_stream(stream, device)), "hbfp_cache_append")
     return held if values else None
 
 
 def cache_read(cache: KvCache, lengths: torch.Tensor, dtype=torch.float32, stream=None):
     """hbfp_cache_read: (keys, values) [batch, heads, capacity, dim], 0 from each length on."""
-    d = cache.desc
+    d, device = cache.desc, cache.k.device
     assert dtype in _TYPES
-    k, v = (_buffer((d.batch, d.heads, d.capacity, d.dim), dtype, cache.k.device, stream) for _ in range(2))
-    _check(_lib.hbfp_cache_read(ctypes.byref(d), _lengths(lengths, d.batch, cache.k.device), _TYPES[dtype], _dev_ptr(k), _dev_ptr(v),
-                                _stream_ptr(stream)), "hbfp_cache_read")
+    k, v = (_buffer((d.batch, d.heads, d.capacity, d.dim), dtype, device, stream) for _ in range(2))
+    _check(_lib.hbfp_cache_read(ctypes.byref(d), _lengths(lengths, d.batch, device), _TYPES[dtype], _ptr(k), _ptr(v),
+                                _raw_stream(stream, device)), "hbfp_cache_read")
     return k, v
 
 
 def cache_attend_workspace(desc: CacheDesc, tokens: int, heads: int, dtype=torch.bfloat16, longest: int = 0) -> int:
-    n = ctypes.c_size_t(0)
-    _check(_lib.hbfp_cache_attend_workspace(ctypes.byref(desc), tokens, heads, _TYPES[dtype], longest, ctypes.byref(n)),
-           "hbfp_cache_attend_workspace")
+    return _attend_bytes(desc.batch, desc.heads, desc.capacity, desc.dim, tokens, heads, _TYPES[dtype], longest)
+
+
+@functools.lru_cache(maxsize=1024)     # of sizes alone; asking the library anew would cost every step of a layer 2 us
+def _attend_bytes(batch: int, kv_heads: int, capacity: int, dim: int, tokens: int, heads: int, dtype: int, longest: int) -> int:
+    n, d = ctypes.c_size_t(0), cache_plan(batch, kv_heads, capacity, dim)
+    _check(_lib.hbfp_cache_attend_workspace(ctypes.byref(d), tokens, heads, dtype, longest, ctypes.byref(n)), "hbfp_cache_attend_workspace")
     return int(n.value)
 
 
@@ -767,21 +783,23 @@ def cache_attend(cache: KvCache, q: torch.Tensor, lengths: torch.Tensor, scale: 
                  longest: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                  workspace: Optional[torch.Tensor] = None, stream=None):
     """hbfp_cache_attend: (out, lse) for q [batch, tokens, query heads, dim]; scale defaults to dim ** -0.5."""
-    d = cache.desc
-    tokens, heads = q.shape[1], q.shape[2]
-    hq = _heads(q, d.batch, tokens, heads, d.dim, cache.k.device)
+    d, device = cache.desc, cache.k.device
+    batch, dim = d.batch, d.dim
+    _, tokens, heads, _ = q.shape
+    hq = _heads(q, batch, tokens, heads, dim, device)
     if out is None:
-        out = _buffer(q.shape, q.dtype, q.device, stream)
+        out = _buffer(q.shape, q.dtype, device, stream)
     if lse is None:
-        lse = _buffer((d.batch, tokens, heads), torch.float32, q.device, stream)
-    assert lse.device == q.device and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:3]
-    ho = _heads(out, d.batch, tokens, heads, d.dim, cache.k.device)
+        lse = _buffer((batch, tokens, heads), torch.float32, device, stream)
+    else:
+        assert lse.device == device and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (batch, tokens, heads)
+    ho = _heads(out, batch, tokens, heads, dim, device)
     if workspace is None:
-        need = cache_attend_workspace(d, tokens, heads, q.dtype, longest)
-        workspace = _buffer((need,), torch.uint8, q.device, stream) if need else None
-    _check(_lib.hbfp_cache_attend(ctypes.byref(d), ctypes.byref(hq), tokens, heads, _lengths(lengths, d.batch, q.device), longest,
-                                  d.dim ** -0.5 if scale is None else scale, 1 if causal else 0, ctypes.byref(ho), _dev_ptr(lse),
-                                  _dev_ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream)),
+        need = _attend_bytes(batch, d.heads, d.capacity, dim, tokens, heads, hq.dtype, longest)
+        workspace = _buffer((need,), torch.uint8, device, stream) if need else None
+    _check(_lib.hbfp_cache_attend(ctypes.byref(d), ctypes.byref(hq), tokens, heads, _lengths(lengths, batch, device), longest,
+                                  dim ** -0.5 if scale is None else scale, 1 if causal else 0, ctypes.byref(ho), _ptr(lse),
+                                  _ptr(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(stream, device)),
            "hbfp_cache_attend")
     return out, lse
 
@@ -791,17 +809,18 @@ def cache_weigh(cache: KvCache, q: torch.Tensor, lse: torch.Tensor, lengths: tor
                 stream=None) -> torch.Tensor:
     """hbfp_cache_weigh: out = decay * weights + the attention weight each cached token received; weights FP32 [batch, heads, n],
     n >= capacity; out defaults to weights (in place)."""
-    d = cache.desc
-    tokens, heads = q.shape[1], q.shape[2]
-    hq = _heads(q, d.batch, tokens, heads, d.dim, cache.k.device)
+    d, device = cache.desc, cache.k.device
+    batch, dim = d.batch, d.dim
+    _, tokens, heads, _ = q.shape
+    hq = _heads(q, batch, tokens, heads, dim, device)
     out = weights if out is None else out
     for t in (weights, out):
-        assert t.device == q.device and t.dtype == torch.float32 and t.is_contiguous() and t.dim() == 3
-        assert t.shape[:2] == (d.batch, d.heads) and t.shape == weights.shape
-    assert lse.device == q.device and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:3]
-    _check(_lib.hbfp_cache_weigh(ctypes.byref(d), ctypes.byref(hq), tokens, heads, _lengths(lengths, d.batch, q.device),
-                                 d.dim ** -0.5 if scale is None else scale, 1 if causal else 0, _dev_ptr(lse), decay, _dev_ptr(weights),
-                                 _dev_ptr(out), weights.shape[2], _stream_ptr(stream)), "hbfp_cache_weigh")
+        assert t.device == device and t.dtype == torch.float32 and t.is_contiguous() and t.shape == weights.shape
+    assert weights.dim() == 3 and weights.shape[0] == batch and weights.shape[1] == d.heads
+    assert lse.device == device and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (batch, tokens, heads)
+    _check(_lib.hbfp_cache_weigh(ctypes.byref(d), ctypes.byref(hq), tokens, heads, _lengths(lengths, batch, device),
+                                 dim ** -0.5 if scale is None else scale, 1 if causal else 0, _ptr(lse), decay, _ptr(weights),
+                                 _ptr(out), weights.shape[2], _raw_stream(stream, device)), "hbfp_cache_weigh")
     return out
 
 
@@ -817,9 +836,9 @@ def cache_evict(cache: KvCache, weights: torch.Tensor, lengths: torch.Tensor, ou
     assert out_weights.shape[:2] == (d.batch, d.heads)
     kept = _buffer((d.batch, d.heads, max(keep, 1)), torch.int32, device, stream)
     new_lengths = _buffer((d.batch,), torch.int32, device, stream)
-    _check(_lib.hbfp_cache_evict(ctypes.byref(d), _dev_ptr(weights), weights.shape[2], _lengths(lengths, d.batch, device), keep, recent,
-                                 ctypes.byref(out.desc), _dev_ptr(out_weights), out_weights.shape[2], _dev_ptr(kept),
-                                 _dev_ptr(new_lengths), _stream_ptr(stream)), "hbfp_cache_evict")
+    _check(_lib.hbfp_cache_evict(ctypes.byref(d), _ptr(weights), weights.shape[2], _lengths(lengths, d.batch, device), keep, recent,
+                                 ctypes.byref(out.desc), _ptr(out_weights), out_weights.shape[2], _ptr(kept),
+                                 _ptr(new_lengths), _raw_stream(stream, device)), "hbfp_cache_evict")
     return kept, new_lengths, out_weights
 
 
@@ -844,8 +863,8 @@ def quant_rows(x: torch.Tensor, stream=None) -> RowCodes:
     _check(_lib.hbfp_rows_plan(x.shape[0], x.shape[1], ctypes.byref(kpad), None), "hbfp_rows_plan")
     codes = _buffer((x.shape[0], kpad.value), torch.int8, x.device, stream)
     scales = _buffer((x.shape[0],), torch.float32, x.device, stream)
-    _check(_lib.hbfp_quant_rows(_dev_ptr(x), _TYPES[x.dtype], x.shape[0], x.shape[1], ld, _dev_ptr(codes), _dev_ptr(scales),
-                                _stream_ptr(stream)), "hbfp_quant_rows")
+    _check(_lib.hbfp_quant_rows(_ptr(x), _TYPES[x.dtype], x.shape[0], x.shape[1], ld, _ptr(codes), _ptr(scales),
+                                _raw_stream(stream, x.device)), "hbfp_quant_rows")
     return RowCodes(codes, scales, x.shape[1])
 
 
@@ -860,6 +879,20 @@ def _product_out(bias, w: RowCodes, rows: int, dtype, device, out, stream):
     return out, _matrix(out)
 
 
+@functools.lru_cache(maxsize=1024)
+def gemm_rows_workspace(rows: int, out_features: int, in_features: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.hbfp_gemm_rows_workspace(rows, out_features, in_features, ctypes.byref(n)), "hbfp_gemm_rows_workspace")
+    return int(n.value)
+
+
+@functools.lru_cache(maxsize=1024)
+def linear_i8_workspace(rows: int, out_features: int, in_features: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.hbfp_linear_i8_workspace(rows, out_features, in_features, ctypes.byref(n)), "hbfp_linear_i8_workspace")
+    return int(n.value)
+
+
 def gemm_rows(a: RowCodes, w: RowCodes, bias: Optional[torch.Tensor] = None, dtype=torch.float32, out: Optional[torch.Tensor] = None,
               workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """hbfp_gemm_rows: y [rows of a, rows of w] = a . w^T (+ bias), rounded once to `dtype`."""
@@ -867,12 +900,11 @@ def gemm_rows(a: RowCodes, w: RowCodes, bias: Optional[torch.Tensor] = None, dty
     m, n, device = a.codes.shape[0], w.codes.shape[0], a.codes.device
     out, ld = _product_out(bias, w, m, dtype if out is None else out.dtype, device, out, stream)
     if workspace is None:
-        need = ctypes.c_size_t(0)
-        _check(_lib.hbfp_gemm_rows_workspace(m, n, a.cols, ctypes.byref(need)), "hbfp_gemm_rows_workspace")
-        workspace = _buffer((need.value,), torch.uint8, device, stream) if need.value else None
-    _check(_lib.hbfp_gemm_rows(_dev_ptr(a.codes), _dev_ptr(a.scales), _dev_ptr(w.codes), _dev_ptr(w.scales), _dev_ptr(bias), m, n, a.cols,
-                               _dev_ptr(out), _TYPES[out.dtype], ld, _dev_ptr(workspace), 0 if workspace is None else workspace.numel(),
-                               _stream_ptr(stream)), "hbfp_gemm_rows")
+        need = gemm_rows_workspace(m, n, a.cols)
+        workspace = _buffer((need,), torch.uint8, device, stream) if need else None
+    _check(_lib.hbfp_gemm_rows(_ptr(a.codes), _ptr(a.scales), _ptr(w.codes), _ptr(w.scales), _ptr(bias), m, n, a.cols,
+                               _ptr(out), _TYPES[out.dtype], ld, _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                               _raw_stream(stream, device)), "hbfp_gemm_rows")
     return out
 
 
@@ -883,9 +915,7 @@ def linear_i8(x: torch.Tensor, w: RowCodes, bias: Optional[torch.Tensor] = None,
     assert k == w.cols
     out, ldy = _product_out(bias, w, m, x.dtype, x.device, out, stream)
     if workspace is None:
-        need = ctypes.c_size_t(0)
-        _check(_lib.hbfp_linear_i8_workspace(m, n, k, ctypes.byref(need)), "hbfp_linear_i8_workspace")
-        workspace = _buffer((need.value,), torch.uint8, x.device, stream)
-    _check(_lib.hbfp_linear_i8(_dev_ptr(x), _TYPES[x.dtype], m, k, ldx, _dev_ptr(w.codes), _dev_ptr(w.scales), _dev_ptr(bias), n,
-                               _dev_ptr(out), ldy, _dev_ptr(workspace), workspace.numel(), _stream_ptr(stream)), "hbfp_linear_i8")
+        workspace = _buffer((linear_i8_workspace(m, n, k),), torch.uint8, x.device, stream)
+    _check(_lib.hbfp_linear_i8(_ptr(x), _TYPES[x.dtype], m, k, ldx, _ptr(w.codes), _ptr(w.scales), _ptr(bias), n,
+                               _ptr(out), ldy, _ptr(workspace), workspace.numel(), _raw_stream(stream, x.device)), "hbfp_linear_i8")
     return out
