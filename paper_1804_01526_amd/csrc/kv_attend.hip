@@ -41,7 +41,7 @@ __device__ __forceinline__ void load_queries(const Heads &q, int64_t b, int key_
     for (int blk = 0; blk < NB; ++blk) {
         const int d0 = 32 * blk + 8 * g, n = real ? dim - d0 : 0;
         float x[8];
-        load8<DT>(q.data, base + d0, n, n >= 8 && q.wide, x);
+        load8<DT>(q.data, base + d0, n, x);
         uint32_t w[4][Pieces<DT>::n];
 #pragma unroll
         for (int i = 0; i < 4; ++i) bf16_pieces2<Pieces<DT>::n>(x[2 * i], x[2 * i + 1], w[i]);

@@ -54,17 +54,20 @@ __device__ __forceinline__ void store_float(void *p, int64_t i, float x) {
     else if (DT == HBFP_BF16) reinterpret_cast<__bf16 *>(p)[i] = (__bf16)x;
     else reinterpret_cast<_Float16 *>(p)[i] = (_Float16)x;
 }
-// eight consecutive elements from i on, of which n (may be <= 0) exist, the others 0; whole: all exist and the address allows wide loads
+// eight consecutive elements from i on, of which n (may be <= 0) exist, the others 0.  Wide loads need no more than the elements' own
+// alignment here.
+typedef float v4f_at __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t v4u_at __attribute__((ext_vector_type(4), aligned(2)));
 template <int DT>
-__device__ __forceinline__ void load8(const void *p, int64_t i, int n, bool whole, float *x) {
-    if (whole) {
+__device__ __forceinline__ void load8(const void *p, int64_t i, int n, float *x) {
+    if (n >= 8) {
         if (DT == HBFP_F32) {
-            const v4f a = *reinterpret_cast<const v4f *>(reinterpret_cast<const float *>(p) + i);
-            const v4f b = *reinterpret_cast<const v4f *>(reinterpret_cast<const float *>(p) + i + 4);
+            const v4f_at a = *reinterpret_cast<const v4f_at *>(reinterpret_cast<const float *>(p) + i);
+            const v4f_at b = *reinterpret_cast<const v4f_at *>(reinterpret_cast<const float *>(p) + i + 4);
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] = a[j], x[4 + j] = b[j];
         } else {
-            const v4u a = *reinterpret_cast<const v4u *>(reinterpret_cast<const uint16_t *>(p) + i);
+            const v4u_at a = *reinterpret_cast<const v4u_at *>(reinterpret_cast<const uint16_t *>(p) + i);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint32_t h = j & 1 ? a[j / 2] >> 16 : a[j / 2] & 0xffffu;

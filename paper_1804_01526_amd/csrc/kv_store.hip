@@ -65,8 +65,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendParams p)
     const bool mine = t >= 0 && t < p.tokens, held = mine && slot >= 0 && slot < p.c.capacity;
     const int d0 = 32 * blk + 8 * g, n = mine ? p.c.dim - d0 : 0;
     float xk[8], xv[8];
-    load8<DT>(p.k.data, b * p.k.sb + t * p.k.st + h * p.k.sh + d0, n, n >= 8 && p.k.wide, xk);
-    load8<DT>(p.v.data, b * p.v.sb + t * p.v.st + h * p.v.sh + d0, n, n >= 8 && p.v.wide, xv);
+    load8<DT>(p.k.data, b * p.k.sb + t * p.k.st + h * p.k.sh + d0, n, xk);
+    load8<DT>(p.v.data, b * p.v.sb + t * p.v.st + h * p.v.sh + d0, n, xv);
     uint32_t ek, ev;
     const uint32_t wk = convert8<DT>(xk, ek), wv = convert8<DT>(xv, ev);
     const uint32_t partner = __shfl_xor(wv, 2);               // dimensions 16 higher (g 0, 1) of the same block and slot

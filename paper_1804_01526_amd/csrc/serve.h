@@ -8,7 +8,6 @@ namespace hbfp {
 struct Heads {
     void *data;
     int64_t sb, st, sh;
-    int32_t wide;             // rows of a head start on 16-byte addresses
 };
 
 struct CacheView {
@@ -60,5 +59,8 @@ struct RowsArgs {
 int launch_quant_rows(const void *src, int dtype, int64_t rows, int64_t cols, int64_t ld, int8_t *codes, float *scales, hipStream_t s);
 size_t gemm_rows_workspace(int64_t M, int64_t N, int64_t kpad);
 int launch_gemm_rows(const RowsArgs &a, void *workspace, hipStream_t s);
+// x converted inside the product: one or two tokens whose codes fit into LDS; a.a and a.sa are not read
+bool linear_fused_ok(int64_t M, int64_t N, int64_t kpad);
+int launch_linear_fused(const RowsArgs &a, const void *x, int64_t ldx, hipStream_t s);
 
 }  // namespace hbfp

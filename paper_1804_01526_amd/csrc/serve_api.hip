@@ -67,11 +67,7 @@ int check_heads(const hbfp_heads *h, int64_t batch, int64_t tokens, int64_t head
     }
     return HBFP_OK;
 }
-Heads heads_of(const hbfp_heads &h) {
-    const uint64_t size = h.dtype == HBFP_F32 ? 4 : 2;
-    const uint64_t at = (uint64_t)(uintptr_t)h.data | (uint64_t)h.stride_batch * size | (uint64_t)h.stride_token * size | (uint64_t)h.stride_head * size;
-    return {h.data, h.stride_batch, h.stride_token, h.stride_head, (at & 15) == 0};
-}
+Heads heads_of(const hbfp_heads &h) { return {h.data, h.stride_batch, h.stride_token, h.stride_head}; }
 
 // tokens and query heads of a call that reads the cache; the rows of a key head have to fit 31 bits
 int check_queries(const hbfp_cache *c, int64_t tokens, int64_t heads) {
@@ -259,7 +255,7 @@ int hbfp_linear_i8_workspace(int64_t M, int64_t N, int64_t K, size_t *bytes) {
     const int rc = check_product(M, N, K);
     if (rc != HBFP_OK || !bytes) return rc != HBFP_OK ? rc : HBFP_ERR_ARG;
     const int64_t kpad = round_up(K, 128);
-    *bytes = align256(gemm_rows_workspace(M, N, kpad)) + align256((size_t)M * kpad) + align256((size_t)M * 4);
+    *bytes = linear_fused_ok(M, N, kpad) ? 0 : align256(gemm_rows_workspace(M, N, kpad)) + align256((size_t)M * kpad) + align256((size_t)M * 4);
     return HBFP_OK;
 }
 
@@ -271,8 +267,12 @@ int hbfp_linear_i8(const void *x, int dtype, int64_t M, int64_t K, int64_t ldx, 
     if ((rc = check_matrix(x, dtype, M, K, ldx)) != HBFP_OK) return rc;
     if ((rc = check_matrix(y, dtype, M, N, ldy)) != HBFP_OK) return rc;
     if (!b || !b_scales || ((uintptr_t)b & 15) || (((uintptr_t)b_scales | (uintptr_t)bias) & 3)) return HBFP_ERR_ARG;
-    if (!workspace || ws_bytes < need || ((uintptr_t)workspace & 255)) return HBFP_ERR_WORKSPACE;
     const int64_t kpad = round_up(K, 128);
+    if (linear_fused_ok(M, N, kpad)) {
+        const RowsArgs r = {nullptr, b, nullptr, b_scales, bias, y, M, N, K, kpad, ldy, dtype};
+        return launch_linear_fused(r, x, ldx, (hipStream_t)stream);
+    }
+    if (!workspace || ws_bytes < need || ((uintptr_t)workspace & 255)) return HBFP_ERR_WORKSPACE;
     int8_t *const codes = (int8_t *)workspace;
     float *const scales = (float *)(codes + align256((size_t)M * kpad));
     void *const rest = (uint8_t *)scales + align256((size_t)M * 4);

@@ -915,7 +915,8 @@ def linear_i8(x: torch.Tensor, w: RowCodes, bias: Optional[torch.Tensor] = None,
     assert k == w.cols
     out, ldy = _product_out(bias, w, m, x.dtype, x.device, out, stream)
     if workspace is None:
-        workspace = _buffer((linear_i8_workspace(m, n, k),), torch.uint8, x.device, stream)
+        need = linear_i8_workspace(m, n, k)
+        workspace = _buffer((need,), torch.uint8, x.device, stream) if need else None
     _check(_lib.hbfp_linear_i8(_ptr(x), _TYPES[x.dtype], m, k, ldx, _ptr(w.codes), _ptr(w.scales), _ptr(bias), n,
-                               _ptr(out), ldy, _ptr(workspace), workspace.numel(), _raw_stream(stream, x.device)), "hbfp_linear_i8")
+                               _ptr(out), ldy, _ptr(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(stream, x.device)), "hbfp_linear_i8")
     return out
