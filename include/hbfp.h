@@ -737,7 +737,8 @@ int hbfp_cache_plan(int64_t batch, int64_t heads, int64_t capacity, int64_t dim,
 /*
  * hbfp_cache_append: converts the new tokens' keys and values and stores them.  k_values, v_values (each may be NULL): bf16
  * [batch][tokens][heads][dim], contiguous, receive the values the cache now holds for them (exact in bf16), 0 for tokens that
- * were not stored.  Inputs must be finite and below 2^127; a block with an Inf or a NaN makes what reads it NaN or Inf.
+ * were not stored.  Inputs must be finite and below 2^127: a token with an Inf or a NaN in its key or its value makes the result of
+ * every query that sees it NaN (and of no other), and the cache's values for it are unspecified.
  * Errors: HBFP_ERR_ARG, HBFP_ERR_FORMAT (dtype), HBFP_ERR_LAYOUT (cache differs from its plan), HBFP_ERR_LAUNCH.
  */
 int hbfp_cache_append(const hbfp_cache *cache, const hbfp_heads *k, const hbfp_heads *v, int64_t tokens, const int32_t *lengths,

@@ -12,23 +12,7 @@
 namespace hbfp {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kWaves = 4;
-
-struct SplitParams {
-    AttendArgs a;
-    float *ml, *o;            // partial results: [batch * heads][chunks][rows] (max, sum) and [..][32 nblk]
-    int32_t rows, tiles, chunk, chunks;
-    float scale2;             // scale * log2(e)
-    uint32_t wgs;
-};
-
-// keys that row `row` (token row / group) of batch entry b may see
-__device__ __forceinline__ int visible(int length, int tokens, int group, int row, int causal, int bound) {
-    const int len = length < 0 ? 0 : length;
-    const int64_t n = causal ? (int64_t)len - tokens + row / group + 1 : (int64_t)len;
-    return n < 0 ? 0 : n > bound ? bound : (int)n;
-}
 
 // a wave's 16 queries as the second operand of S^T = K Q^T: lane c + 16 g has dimensions 32 blk + 8 g .. + 7 of query c
 template <int NB, int DT>
@@ -64,28 +48,6 @@ __device__ __forceinline__ v4f scores16(const uint32_t (&w)[NB], const uint32_t 
         for (int p = NP - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[p][blk], s, 0, 0, 0);
     }
     return s;
-}
-
-template <int N>
-__device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N]) {
-    if (N % 4 == 0) {
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i) {
-            const v4u x = reinterpret_cast<const v4u *>(p)[i];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[4 * i + k] = x[k];
-        }
-    } else if (N % 2 == 0) {
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            const v2u x = reinterpret_cast<const v2u *>(p)[i];
-            w[2 * i] = x[0];
-            w[2 * i + 1] = x[1];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
-    }
 }
 
 // One step of KS keys from key0 on.  MASK: some of the wave's queries do not see all of them.
@@ -250,7 +212,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const SplitParams p) {
     const int64_t bh = blockIdx.x / p.rows;
     const int64_t b = bh / cache.heads;
     const int key_head = (int)(bh % cache.heads);
-    const int tile = row / 16, last_row = 16 * tile + 15 < p.rows ? 16 * tile + 15 : p.rows - 1;
+    const int end_row = (row / p.tile_rows + 1) * p.tile_rows, last_row = end_row < p.rows ? end_row - 1 : p.rows - 1;
     const int most = visible(p.a.lengths[b], p.a.tokens, p.a.group, last_row, p.a.causal, p.a.longest);
     const int n = (most + p.chunk - 1) / p.chunk;             // chunks that wrote
     const int quads = 8 * cache.nblk, parts = 256 / quads;    // groups of four dimensions; at most 64
@@ -294,15 +256,17 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const SplitParams p) {
 }
 
 // Chunks of keys: enough workgroups to fill the chip several times over, none shorter than a step of its four waves.
-SplitParams split_of(const AttendArgs &a) {
+SplitParams split_of(const AttendArgs &a, int dtype) {
     SplitParams p = {};
     p.a = a;
     p.rows = a.tokens * a.group;
-    p.tiles = (int32_t)ceil_div(p.rows, 16);
+    const bool prompt = cache_prompt_ok(a, dtype);
+    p.tile_rows = prompt ? (int32_t)cache_prompt_rows(a) : 16;
+    p.tiles = (int32_t)ceil_div(p.rows, p.tile_rows);
     p.scale2 = a.scale * kLog2e;
     const int64_t heads = (int64_t)a.c.batch * a.c.heads * p.tiles;
-    const int64_t step = kWaves * (a.c.nblk <= 4 ? 64 : 32);
-    const int64_t want = ceil_div(2048, heads);
+    const int64_t step = prompt ? 512 : kWaves * (a.c.nblk <= 4 ? 64 : 32);
+    const int64_t want = ceil_div(prompt ? 512 : 2048, heads);
     p.chunk = (int32_t)round_up(ceil_div(a.longest, want), step);
     p.chunks = (int32_t)ceil_div(a.longest, p.chunk);
     return p;
@@ -430,19 +394,19 @@ int launch_weigh_of(const WeighParams &p, hipStream_t s) {
 }  // namespace
 
 size_t cache_attend_workspace(const AttendArgs &a, int dtype) {
-    (void)dtype;
-    return split_floats(split_of(a)) * 4;
+    return split_floats(split_of(a, dtype)) * 4;
 }
 
 int launch_cache_attend(const AttendArgs &a, int dtype, hipStream_t s) {
-    SplitParams p = split_of(a);
+    SplitParams p = split_of(a, dtype);
     const int64_t heads = (int64_t)a.c.batch * a.c.heads;
     const int64_t wgs = heads * p.tiles * p.chunks, rows = heads * p.rows;
     if (wgs > 0x7fffffff || rows > 0x7fffffff) return HBFP_ERR_ARG;
     p.wgs = (uint32_t)wgs;
     p.o = a.ws;
     p.ml = a.ws ? a.ws + heads * p.chunks * p.rows * 32 * a.c.nblk : nullptr;
-    int rc = dtype == HBFP_F32 ? launch_split_of<HBFP_F32>(p, s) : dtype == HBFP_BF16 ? launch_split_of<HBFP_BF16>(p, s) : launch_split_of<HBFP_F16>(p, s);
+    int rc = cache_prompt_ok(a, dtype) ? launch_cache_prompt(p, dtype, s)
+             : dtype == HBFP_F32 ? launch_split_of<HBFP_F32>(p, s) : dtype == HBFP_BF16 ? launch_split_of<HBFP_BF16>(p, s) : launch_split_of<HBFP_F16>(p, s);
     if (rc != HBFP_OK || p.chunks == 1) return rc;
     void (*const join)(SplitParams) = dtype == HBFP_F32    ? &cache_join_kernel<HBFP_F32>
                                       : dtype == HBFP_BF16 ? &cache_join_kernel<HBFP_BF16>

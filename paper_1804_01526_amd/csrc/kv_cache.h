@@ -15,6 +15,15 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// keys that row `row` (token row / group) of batch entry b may see
+__device__ __forceinline__ int visible(int length, int tokens, int group, int row, int causal, int bound) {
+    const int len = length < 0 ? 0 : length;
+    const int64_t n = causal ? (int64_t)len - tokens + row / group + 1 : (int64_t)len;
+    return n < 0 ? 0 : n > bound ? bound : (int)n;
+}
+
 // ---- nibbles -> numbers.  A nibble is sign and magnitude, so that one byte permute looks four magnitudes up in a table of
 // eight FP8 (E4M3) numbers, n / 4, and the sign is the fourth bit moved to the eighth: four instructions for the four low or
 // the four high nibbles of a word.  The conversion FP8 -> bf16 multiplies by a power of two, whose FP32 exponent field is
@@ -80,9 +89,50 @@ __device__ __forceinline__ void load8(const void *p, int64_t i, int n, float *x)
     for (int j = 0; j < 8; ++j) x[j] = j < n ? load_as_float<DT>(p, i + j) : 0.0f;
 }
 
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N]) {
+    if (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const v4u x = reinterpret_cast<const v4u *>(p)[i];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[4 * i + k] = x[k];
+        }
+    } else if (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const v2u x = reinterpret_cast<const v2u *>(p)[i];
+            w[2 * i] = x[0];
+            w[2 * i + 1] = x[1];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+    }
+}
+
 __device__ __forceinline__ uint32_t bf16_bits2(float a, float b) {
     const v2bf r = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(uint32_t, r);
+}
+// four consecutive elements from i on, of which n (may be <= 0) exist
+template <int DT>
+__device__ __forceinline__ void store4(void *p, int64_t i, int n, const float *x) {
+    typedef uint32_t v2u_at __attribute__((ext_vector_type(2), aligned(2)));
+    if (n >= 4) {
+        if (DT == HBFP_F32) {
+            *reinterpret_cast<v4f_at *>(reinterpret_cast<float *>(p) + i) = v4f_at{x[0], x[1], x[2], x[3]};
+        } else if (DT == HBFP_BF16) {
+            *reinterpret_cast<v2u_at *>(reinterpret_cast<uint16_t *>(p) + i) = v2u_at{bf16_bits2(x[0], x[1]), bf16_bits2(x[2], x[3])};
+        } else {
+            typedef _Float16 v4h_at __attribute__((ext_vector_type(4), aligned(2)));
+            *reinterpret_cast<v4h_at *>(reinterpret_cast<_Float16 *>(p) + i) = v4h_at{(_Float16)x[0], (_Float16)x[1], (_Float16)x[2], (_Float16)x[3]};
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (j < n) store_float<DT>(p, i + j, x[j]);
 }
 // x as a sum of N bf16 numbers, the first N * 8 bits of it: piece p of two values
 template <int N>

@@ -69,6 +69,10 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendParams p)
     load8<DT>(p.v.data, b * p.v.sb + t * p.v.st + h * p.v.sh + d0, n, xv);
     uint32_t ek, ev;
     const uint32_t wk = convert8<DT>(xk, ek), wv = convert8<DT>(xv, ev);
+    // an Inf or a NaN in a value is marked in the key's exponent, which makes the score of whoever sees the token NaN: the kernels
+    // then never meet a value that is not finite, and a weight of 0 silences any value
+    ek = ev == 255u ? 255u : ek;
+    ev = ev == 255u ? 254u : ev;
     const uint32_t partner = __shfl_xor(wv, 2);               // dimensions 16 higher (g 0, 1) of the same block and slot
     if (held) {
         uint8_t *kc = p.c.k + bh * p.c.head_codes, *vc = p.c.v + bh * p.c.head_codes;

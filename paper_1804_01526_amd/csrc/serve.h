@@ -27,6 +27,15 @@ struct AttendArgs {
     float *ws;
 };
 
+// An attention call as its kernels see it: query rows (token, head of the group) of every key head in tiles, keys in chunks
+struct SplitParams {
+    AttendArgs a;
+    float *ml, *o;            // partial results, [batch * heads][chunks][rows]: (max, sum) and [32 nblk]
+    int32_t rows, tile_rows, tiles, chunk, chunks;
+    float scale2;             // scale * log2(e)
+    uint32_t wgs;
+};
+
 // kv_store.hip
 int launch_cache_append(const CacheView &c, const Heads &k, const Heads &v, int dtype, int64_t tokens, const int32_t *lengths,
                         void *k_values, void *v_values, hipStream_t s);
@@ -36,6 +45,10 @@ int launch_cache_evict(const CacheView &src, const float *w, int64_t ld, const i
 // kv_attend.hip
 size_t cache_attend_workspace(const AttendArgs &a, int dtype);
 int launch_cache_attend(const AttendArgs &a, int dtype, hipStream_t s);
+// kv_prompt.hip: many rows a key head
+bool cache_prompt_ok(const AttendArgs &a, int dtype);
+int64_t cache_prompt_rows(const AttendArgs &a);
+int launch_cache_prompt(const SplitParams &p, int dtype, hipStream_t s);
 struct WeighArgs {
     CacheView c;
     Heads q;
