@@ -264,6 +264,7 @@ SplitParams split_of(const AttendArgs &a, int dtype) {
     p.tile_rows = prompt ? (int32_t)cache_prompt_rows(a) : 16;
     p.tiles = (int32_t)ceil_div(p.rows, p.tile_rows);
     p.scale2 = a.scale * kLog2e;
+    if (prompt) p.scale2 = p.scale2 == 0.0f ? 1.2e-38f : p.scale2 < 0.0f ? -p.scale2 : p.scale2;     // (0 times a masked -infinity is no number)
     const int64_t heads = (int64_t)a.c.batch * a.c.heads * p.tiles;
     const int64_t step = prompt ? 512 : kWaves * (a.c.nblk <= 4 ? 64 : 32);
     const int64_t want = ceil_div(prompt ? 512 : 2048, heads);

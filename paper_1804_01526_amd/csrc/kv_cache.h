@@ -40,6 +40,8 @@ template <bool HIGH>
 __device__ __forceinline__ uint32_t bf16_pair(uint32_t fp8, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(fp8, scale, HIGH));
 }
+// the same scale for the FP8 conversion, which looks at nothing but the exponent field: the byte `j` of a word moved there
+__device__ __forceinline__ float conversion_scale(uint32_t word, int j) { return __uint_as_float(j < 3 ? word << (23 - 8 * j) : word >> 1); }
 // the 2^(Eb - 127) of the exponent byte `j` of a word
 __device__ __forceinline__ float exponent_scale(uint32_t word, int j) { return __uint_as_float(((word >> (8 * j)) & 0xffu) << 23); }
 

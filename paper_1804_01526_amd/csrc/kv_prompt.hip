@@ -14,6 +14,7 @@ namespace {
 struct No { static constexpr bool value = false; };
 struct Yes { static constexpr bool value = true; };
 constexpr int kTile = 64;                  // keys
+constexpr float kSlack = 6.0f;
 constexpr int kValuePitch = kTile * 2 + 16;  // bytes of a row of transposed values: 16 more than its keys, so that rows differ in banks
 template <int NB> struct PromptLds {
     static constexpr int kKeyPitch = 64 * NB + 16, kKeys = kTile * kKeyPitch, kValues = 32 * NB * kValuePitch;
@@ -77,6 +78,9 @@ __global__ __launch_bounds__(64 * W, 2) void cache_prompt_kernel(const SplitPara
         const int d0 = 16 * ks + 8 * h;
         float x[8];
         load8<DT>(p.a.q.data, q_at + d0, row < p.rows ? cache.dim - d0 : 0, x);
+        if (p.a.scale < 0.0f)                               // scale2 is the magnitude
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = -x[i];
         uint32_t w[4][NP];
 #pragma unroll
         for (int i = 0; i < 4; ++i) bf16_pieces2<NP>(x[2 * i], x[2 * i + 1], w[i]);
@@ -112,9 +116,10 @@ __global__ __launch_bounds__(64 * W, 2) void cache_prompt_kernel(const SplitPara
             const int item = wave + W * i, e = 64 * (item & 3) + lane;
             if (item < 4) {
                 uint8_t *const dst = kb + (e >> 2) * L::kKeyPitch + (e & 3) * 16;
+                const int down = 8 * ((e >> 2) & 3);
 #pragma unroll
                 for (int blk = 0; blk < NB; ++blk)
-                    *reinterpret_cast<v8bf *>(dst + blk * 64) = key_values(raw[i].w[blk], exponent_scale(raw[i].e[blk], (e >> 2) & 3));
+                    *reinterpret_cast<v8bf *>(dst + blk * 64) = key_values(raw[i].w[blk], conversion_scale(raw[i].e[blk] >> down, 0));
             } else {
                 const int j4 = e >> 4, c = e & 15;
                 // nothing past the stored tokens may be infinite: a weight of 0 has to silence it
@@ -124,7 +129,7 @@ __global__ __launch_bounds__(64 * W, 2) void cache_prompt_kernel(const SplitPara
 #pragma unroll
                 for (int blk = 0; blk < NB; ++blk) {
                     const uint32_t x = raw[i].e[blk] & mask, lo = fp8_of_low(raw[i].w[blk]), hi = fp8_of_high(raw[i].w[blk]);
-                    const float s0 = exponent_scale(x, 0), s1 = exponent_scale(x, 1), s2 = exponent_scale(x, 2), s3 = exponent_scale(x, 3);
+                    const float s0 = conversion_scale(x, 0), s1 = conversion_scale(x, 1), s2 = conversion_scale(x, 2), s3 = conversion_scale(x, 3);
                     const v2u a = {bf16_pair2<false>(lo, s0, s1), bf16_pair2<true>(lo, s2, s3)};
                     const v2u z = {bf16_pair2<false>(hi, s0, s1), bf16_pair2<true>(hi, s2, s3)};
                     *reinterpret_cast<v2u *>(dst + 32 * blk * kValuePitch) = a;
@@ -147,30 +152,31 @@ __global__ __launch_bounds__(64 * W, 2) void cache_prompt_kernel(const SplitPara
         const uint8_t *const vb = lds + buffer * L::kBuffer + L::kKeys + l32 * kValuePitch + h * 16;
         v16f s[2];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int x = 0; x < 16; ++x) s[kt][x] = 0.0f;
 #pragma unroll
-            for (int ks = 0; ks < 2 * NB; ++ks) {
+        for (int ks = 0; ks < 2 * NB; ++ks)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
                 const v8bf a = *reinterpret_cast<const v8bf *>(kb + kt * 32 * L::kKeyPitch + ks * 32);
 #pragma unroll
                 for (int n = NP - 1; n >= 0; --n) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[n][ks], s[kt], 0, 0, 0);
             }
-        }
         float top = -INFINITY;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
-                s[kt][x] *= p.scale2;
                 if (MASK) s[kt][x] = key0 + 32 * kt + 8 * (x >> 2) + 4 * h + (x & 3) < limit ? s[kt][x] : -INFINITY;
                 top = fmaxf(top, s[kt][x]);
             }
         const v2u sw = __builtin_bit_cast(v2u, __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false));
-        top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-        const float m_new = fmaxf(m, top), from = m_new == -INFINITY ? 0.0f : m_new;
-        if (__any(m_new > m)) {
-            const float shrink = __builtin_amdgcn_exp2f(m - from);
+        top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * p.scale2;
+        // m is the largest score up to a factor of 2^kSlack in its exponential: among 32 queries a new largest score turns up in most
+        // tiles, one that much larger hardly ever after the first
+        if (__any(top > m + kSlack)) {
+            const float m_new = fmaxf(m, top), shrink = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
             l *= shrink;
 #pragma unroll
             for (int i = 0; i < NB; ++i)
@@ -178,6 +184,7 @@ __global__ __launch_bounds__(64 * W, 2) void cache_prompt_kernel(const SplitPara
                 for (int x = 0; x < 16; ++x) o[i][x] *= shrink;
             m = m_new;
         }
+        const float from = m == -INFINITY ? 0.0f : m;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -185,8 +192,8 @@ __global__ __launch_bounds__(64 * W, 2) void cache_prompt_kernel(const SplitPara
                 uint32_t w[4][NP];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float x = __builtin_amdgcn_exp2f(s[kt][8 * ks + 2 * i] - from);
-                    const float y = __builtin_amdgcn_exp2f(s[kt][8 * ks + 2 * i + 1] - from);
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][8 * ks + 2 * i], p.scale2, -from));
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][8 * ks + 2 * i + 1], p.scale2, -from));
                     l += x + y;
                     bf16_pieces2<NP>(x, y, w[i]);
                 }
@@ -207,15 +214,33 @@ __global__ __launch_bounds__(64 * W, 2) void cache_prompt_kernel(const SplitPara
         deliver(begin, 0);
         if (begin + kTile < end) request(begin + kTile);
         __syncthreads();
-        int buffer = 0;
-        for (int key0 = begin; key0 < end; key0 += kTile, buffer ^= 1) {
+        // the tiles that all of the wave's queries see, those that some see, those that are for the other waves: a loop each, so that
+        // the accumulators stay where they are; every wave passes the same number of barriers
+        int key0 = begin, buffer = 0;
+        const auto prepare = [&]() {
             if (key0 + kTile < end) {
                 deliver(key0 + kTile, buffer ^ 1);
                 if (key0 + 2 * kTile < end) request(key0 + 2 * kTile);
             }
-            if (key0 + kTile <= wave_least) multiply(key0, buffer, No());
-            else if (key0 < wave_most) multiply(key0, buffer, Yes());
+        };
+        const auto next = [&]() {
             __syncthreads();
+            key0 += kTile;
+            buffer ^= 1;
+        };
+        while (key0 < end && key0 + kTile <= wave_least) {
+            prepare();
+            multiply(key0, buffer, No());
+            next();
+        }
+        while (key0 < end && key0 < wave_most) {
+            prepare();
+            multiply(key0, buffer, Yes());
+            next();
+        }
+        while (key0 < end) {
+            prepare();
+            next();
         }
     }
     {
