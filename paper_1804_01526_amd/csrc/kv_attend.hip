@@ -43,7 +43,7 @@ __device__ __forceinline__ v4f scores16(const uint32_t (&w)[NB], const uint32_t 
     v4f s = {0, 0, 0, 0};
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk) {
-        const v8bf k = key_values(w[blk], exponent_scale(e[blk], j));
+        const v8bf k = key_values(w[blk], conversion_scale(e[blk] >> (8 * j), 0));
 #pragma unroll
         for (int p = NP - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[p][blk], s, 0, 0, 0);
     }
@@ -194,65 +194,79 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 4 ? 2 : 1) void cache_attend_ker
         } else {
             const int tok = grow / p.a.group, h = key_head * p.a.group + grow % p.a.group;
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            const int64_t dst = b * p.a.out.sb + tok * p.a.out.st + h * p.a.out.sh + d;
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-                if (d + x < cache.dim) store_float<DT>(p.a.out.data, dst + x, acc[x] * inv);
+            const float out4[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+            store4<DT>(p.a.out.data, b * p.a.out.sb + tok * p.a.out.st + h * p.a.out.sh + d, cache.dim - d, out4);
             if (d == 0) p.a.lse[(b * p.a.tokens + tok) * p.a.heads + h] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
         }
     }
 }
 
-// Joins the chunks of one row: sums in the chunks' order within each of the workgroup's parts, then over the parts.
-template <int DT>
-__global__ __launch_bounds__(256) void cache_join_kernel(const SplitParams p) {
-    __shared__ float lds[256 * 4 + 2 * 256];
+// Joins the chunks of the rows: `parts` groups of 8 nblk threads (four dimensions each) share a row's chunks, each in their order,
+// and are joined in theirs.  The largest maximum first, so that no chunk waits for the one before it.
+template <int DT, int THREADS>
+__global__ __launch_bounds__(THREADS) void cache_join_kernel(const SplitParams p, int parts) {
+    __shared__ v4f lds[THREADS];
+    __shared__ float lds_l[THREADS];
     const CacheView &cache = p.a.c;
-    const int row = (int)(blockIdx.x % p.rows);
-    const int64_t bh = blockIdx.x / p.rows;
-    const int64_t b = bh / cache.heads;
+    const int quads = 8 * cache.nblk, per_row = quads * parts, rows_here = THREADS / per_row;
+    const int t = threadIdx.x, sub = t / per_row, part = t % per_row / quads, d = 4 * (t % per_row % quads);
+    const int64_t at = (int64_t)blockIdx.x * rows_here + sub;
+    const bool real = sub < rows_here && at < (int64_t)cache.batch * cache.heads * p.rows;
+    const int row = real ? (int)(at % p.rows) : 0;
+    const int64_t bh = real ? at / p.rows : 0, b = bh / cache.heads;
     const int key_head = (int)(bh % cache.heads);
     const int end_row = (row / p.tile_rows + 1) * p.tile_rows, last_row = end_row < p.rows ? end_row - 1 : p.rows - 1;
     const int most = visible(p.a.lengths[b], p.a.tokens, p.a.group, last_row, p.a.causal, p.a.longest);
-    const int n = (most + p.chunk - 1) / p.chunk;             // chunks that wrote
-    const int quads = 8 * cache.nblk, parts = 256 / quads;    // groups of four dimensions; at most 64
-    const int t = threadIdx.x, part = t / quads, d = 4 * (t % quads);
-    float m = -INFINITY, l = 0.0f;
-    v4f acc = {0, 0, 0, 0};
-    if (part < parts)
-        for (int i = part; i < n; i += parts) {
-            const int64_t slot = (bh * p.chunks + i) * p.rows + row;
-            const float mi = p.ml[2 * slot], li = p.ml[2 * slot + 1];
-            const v4f oi = *reinterpret_cast<const v4f *>(p.o + slot * 4 * quads + d);
-            const float top = fmaxf(m, mi), from = top == -INFINITY ? 0.0f : top;
-            const float f0 = __builtin_amdgcn_exp2f(m - from), f1 = __builtin_amdgcn_exp2f(mi - from);
-            l = l * f0 + li * f1;
-            acc = acc * f0 + oi * f1;
-            m = top;
-        }
-    float *const lds_m = lds + 1024, *const lds_l = lds_m + 256;
-    *reinterpret_cast<v4f *>(lds + 4 * t) = acc;
-    lds_m[t] = m;
-    lds_l[t] = l;
-    __syncthreads();
-    if (t >= quads) return;
+    const int n = real ? (most + p.chunk - 1) / p.chunk : 0;  // chunks that wrote
+    const int64_t first = bh * p.chunks * p.rows + row;
     float top = -INFINITY;
-    for (int i = 0; i < parts; ++i) top = fmaxf(top, lds_m[i * quads + t]);
-    const float from = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f;
-    acc = v4f{0, 0, 0, 0};
-    for (int i = 0; i < parts; ++i) {
-        const float f = __builtin_amdgcn_exp2f(lds_m[i * quads + t] - from);
-        sum += f * lds_l[i * quads + t];
-        acc += f * *reinterpret_cast<const v4f *>(lds + 4 * (i * quads + t));
+#pragma unroll 4
+    for (int i = part; i < n; i += parts) top = fmaxf(top, p.ml[2 * (first + (int64_t)i * p.rows)]);
+    if (parts > 1) {
+        lds_l[t] = top;
+        __syncthreads();
+        if (sub < rows_here)
+            for (int i = 0; i < parts; ++i) top = fmaxf(top, lds_l[sub * per_row + i * quads + d / 4]);
+        __syncthreads();
     }
+    const float from = top == -INFINITY ? 0.0f : top;
+    float l = 0.0f;
+    v4f acc = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int i = part; i < n; i += parts) {
+        const int64_t slot = first + (int64_t)i * p.rows;
+        const float f = __builtin_amdgcn_exp2f(p.ml[2 * slot] - from);
+        l += f * p.ml[2 * slot + 1];
+        acc += f * *reinterpret_cast<const v4f *>(p.o + slot * 4 * quads + d);
+    }
+    if (parts > 1) {
+        lds[t] = acc;
+        lds_l[t] = l;
+        __syncthreads();
+        if (part != 0) return;
+        for (int i = 1; i < parts; ++i) {
+            if (sub < rows_here) {
+                acc += lds[t + i * quads];
+                l += lds_l[t + i * quads];
+            }
+        }
+    }
+    if (!real) return;
     const int tok = row / p.a.group, h = key_head * p.a.group + row % p.a.group;
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const int64_t dst = b * p.a.out.sb + tok * p.a.out.st + h * p.a.out.sh + d;
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-        if (d + x < cache.dim) store_float<DT>(p.a.out.data, dst + x, acc[x] * inv);
-    if (t == 0) p.a.lse[(b * p.a.tokens + tok) * p.a.heads + h] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float r[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+    store4<DT>(p.a.out.data, b * p.a.out.sb + tok * p.a.out.st + h * p.a.out.sh + d, cache.dim - d, r);
+    if (d == 0) p.a.lse[(b * p.a.tokens + tok) * p.a.heads + h] = l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;
+}
+template <int DT>
+int launch_join(const SplitParams &p, hipStream_t s) {
+    const int quads = 8 * p.a.c.nblk, threads = p.chunks > 64 ? 1024 : 256, most = threads / quads;
+    const int parts = p.chunks <= 4 ? 1 : (int)ceil_div(p.chunks, 4) < most ? (int)ceil_div(p.chunks, 4) : most;
+    const int64_t wgs = ceil_div((int64_t)p.a.c.batch * p.a.c.heads * p.rows, threads / (quads * parts));
+    if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
+    if (threads == 1024) hipLaunchKernelGGL((cache_join_kernel<DT, 1024>), dim3((unsigned)wgs), dim3(1024), 0, s, p, parts);
+    else hipLaunchKernelGGL((cache_join_kernel<DT, 256>), dim3((unsigned)wgs), dim3(256), 0, s, p, parts);
+    return launch_status();
 }
 
 // Chunks of keys: enough workgroups to fill the chip several times over, none shorter than a step of its four waves.
@@ -300,13 +314,27 @@ int launch_split_of(const SplitParams &p, hipStream_t s) {
 }
 
 // ---- accumulated weights.  A wave turns 64 keys into bf16 numbers once and meets every query of the key head with them; a
-// lane's sums over its query columns are exchanged over the 16 lanes at the end.
+// lane's sums over its query columns are exchanged over the 16 lanes at the end.  A wave walks over kWeighGroups such groups, the
+// words of the next on their way; queries that fit one tile stay in registers.
+constexpr int kWeighGroups = 4;
 struct WeighParams {
     WeighArgs a;
     int32_t rows, tiles;
     float scale2;
-    int64_t units;               // batch * heads * groups of 64 slots
+    int64_t units;               // batch * heads * walks
 };
+
+// of 2 HALF values the lanes c with that bit keep the upper half and the others the lower, joined with those of lane c ^ HALF (a function
+// of its own: as a loop over the halves it kept the array in registers only by comparing every index, 50 us instead of 14)
+template <int HALF>
+__device__ __forceinline__ void halve(float (&sum)[16], int c) {
+    const bool upper = (c & HALF) != 0;
+#pragma unroll
+    for (int i = 0; i < HALF; ++i) {
+        const float mine = upper ? sum[i + HALF] : sum[i], give = upper ? sum[i] : sum[i + HALF];
+        sum[i] = mine + __shfl_xor(give, HALF);
+    }
+}
 
 template <int NB, int DT>
 __global__ __launch_bounds__(256) void cache_weigh_kernel(const WeighParams p) {
@@ -316,69 +344,82 @@ __global__ __launch_bounds__(256) void cache_weigh_kernel(const WeighParams p) {
     const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (unit >= p.units) return;
     const int64_t heads = (int64_t)cache.batch * cache.heads, bh = unit % heads;
-    const int key0 = (int)(unit / heads) * 64;
+    const int begin = (int)(unit / heads) * 64 * kWeighGroups, bound = cache.capacity;
+    const int end = begin + 64 * kWeighGroups < bound ? begin + 64 * kWeighGroups : bound;
     const int64_t b = bh / cache.heads;
     const int key_head = (int)(bh % cache.heads);
-    const int length = p.a.lengths[b], bound = cache.capacity;
+    const int length = p.a.lengths[b];
     const int held = visible(length, p.a.tokens, p.a.group, 0, 0, bound);
-    // this lane's result: value index c of its 16, key 16 (c / 4) + 4 g + c % 4
-    const int key = key0 + 16 * (c >> 2) + 4 * g + (c & 3);
-    const int64_t at = bh * p.a.ld + key;
-    if (key0 >= held) {
-        if (key < bound) p.a.w_out[at] = 0.0f;
-        return;
-    }
-    const float before = key < held ? p.a.w_in[at] : 0.0f;
+    // this lane's result of a group: value index c of its 16, key 16 (c / 4) + 4 g + c % 4
+    const int own = 16 * (c >> 2) + 4 * g + (c & 3);
+    float *const w_out = p.a.w_out + bh * p.a.ld;
+    const float *const w_in = p.a.w_in + bh * p.a.ld;
     const uint8_t *k = cache.k + bh * cache.head_codes, *ke = cache.ke + bh * cache.head_exps;
-    v8bf kf[4][NB];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        uint32_t w[NB], e[NB];
-        load_words<NB>(k + (uint32_t)((key0 + 16 * t + c) * 16 + g * 4) * NB, w);
-        load_words<NB>(ke + (uint32_t)((key0 + 16 * t) / 4 + c / 4) * 4 * NB, e);
-#pragma unroll
-        for (int blk = 0; blk < NB; ++blk) kf[t][blk] = key_values(w[blk], exponent_scale(e[blk], c & 3));
-    }
-    float sum[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
-    for (int tile = 0; tile < p.tiles; ++tile) {
-        const int last_row = 16 * tile + 15 < p.rows ? 16 * tile + 15 : p.rows - 1;
-        if (visible(length, p.a.tokens, p.a.group, last_row, p.a.causal, bound) <= key0) continue;
+    v8bf q[NP][NB];
+    int limit = 0;
+    float lse2 = 0.0f;
+    const auto load_tile = [&](int tile) {
         const int row = 16 * tile + c;
-        int limit = 0;
-        float lse2 = 0.0f;
+        limit = 0;
         if (row < p.rows) {
             limit = visible(length, p.a.tokens, p.a.group, row, p.a.causal, bound);
             lse2 = p.a.lse[(b * p.a.tokens + row / p.a.group) * p.a.heads + key_head * p.a.group + row % p.a.group] * kLog2e;
         }
-        v8bf q[NP][NB];
         load_queries<NB, DT>(p.a.q, b, key_head, p.a.group, row, p.rows, cache.dim, g, q);
+    };
+    uint32_t w[4][NB], e[4][NB];
+    float before = 0.0f;
+    const auto request = [&](int key0) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            v4f s = {0, 0, 0, 0};
+            load_words<NB>(k + (uint32_t)((key0 + 16 * t + c) * 16 + g * 4) * NB, w[t]);
+            load_words<NB>(ke + (uint32_t)((key0 + 16 * t) / 4 + c / 4) * 4 * NB, e[t]);
+        }
+        before = key0 + own < held ? w_in[key0 + own] : 0.0f;
+    };
+    int key0 = begin;
+    if (key0 < held) {
+        request(key0);
+        if (p.tiles == 1) load_tile(0);
+    }
+    for (; key0 < end && key0 < held; key0 += 64) {
+        v8bf kf[4][NB];
 #pragma unroll
-            for (int blk = 0; blk < NB; ++blk)
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int i = NP - 1; i >= 0; --i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][blk], q[i][blk], s, 0, 0, 0);
+            for (int blk = 0; blk < NB; ++blk) kf[t][blk] = key_values(w[t][blk], conversion_scale(e[t][blk] >> (8 * (c & 3)), 0));
+        const float old = before;
+        if (key0 + 64 < end && key0 + 64 < held) request(key0 + 64);
+        float sum[16];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float x = __builtin_amdgcn_exp2f(s[i] * p.scale2 - lse2);
-                sum[4 * t + i] += key0 + 16 * t + 4 * g + i < limit ? x : 0.0f;
+        for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
+        for (int tile = 0; tile < p.tiles; ++tile) {
+            const int last_row = 16 * tile + 15 < p.rows ? 16 * tile + 15 : p.rows - 1;
+            if (visible(length, p.a.tokens, p.a.group, last_row, p.a.causal, bound) <= key0) continue;
+            if (p.tiles > 1) load_tile(tile);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                v4f s = {0, 0, 0, 0};
+#pragma unroll
+                for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+                    for (int i = NP - 1; i >= 0; --i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][blk], q[i][blk], s, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = __builtin_amdgcn_exp2f(s[i] * p.scale2 - lse2);
+                    sum[4 * t + i] += key0 + 16 * t + 4 * g + i < limit ? x : 0.0f;
+                }
             }
         }
+        // over the 16 lanes of a row: each exchange halves the values a lane carries
+        halve<8>(sum, c);
+        halve<4>(sum, c);
+        halve<2>(sum, c);
+        halve<1>(sum, c);
+        if (key0 + own < bound) w_out[key0 + own] = key0 + own < held ? p.a.decay * old + sum[0] : 0.0f;
     }
-    // over the 16 lanes of a row: each exchange halves the values a lane carries
-#pragma unroll
-    for (int half = 8; half >= 1; half >>= 1) {
-        const bool upper = (c & half) != 0;
-#pragma unroll
-        for (int i = 0; i < half; ++i) {
-            const float keep = upper ? sum[i + half] : sum[i], give = upper ? sum[i] : sum[i + half];
-            sum[i] = keep + __shfl_xor(give, half);
-        }
-    }
-    if (key < bound) p.a.w_out[at] = key < held ? p.a.decay * before + sum[0] : 0.0f;
+    for (; key0 < end; key0 += 64)
+        if (key0 + lane < bound) w_out[key0 + lane] = 0.0f;
 }
 
 template <int DT>
@@ -409,11 +450,7 @@ int launch_cache_attend(const AttendArgs &a, int dtype, hipStream_t s) {
     int rc = cache_prompt_ok(a, dtype) ? launch_cache_prompt(p, dtype, s)
              : dtype == HBFP_F32 ? launch_split_of<HBFP_F32>(p, s) : dtype == HBFP_BF16 ? launch_split_of<HBFP_BF16>(p, s) : launch_split_of<HBFP_F16>(p, s);
     if (rc != HBFP_OK || p.chunks == 1) return rc;
-    void (*const join)(SplitParams) = dtype == HBFP_F32    ? &cache_join_kernel<HBFP_F32>
-                                      : dtype == HBFP_BF16 ? &cache_join_kernel<HBFP_BF16>
-                                                           : &cache_join_kernel<HBFP_F16>;
-    hipLaunchKernelGGL(join, dim3((unsigned)rows), dim3(256), 0, s, p);
-    return launch_status();
+    return dtype == HBFP_F32 ? launch_join<HBFP_F32>(p, s) : dtype == HBFP_BF16 ? launch_join<HBFP_BF16>(p, s) : launch_join<HBFP_F16>(p, s);
 }
 
 int launch_cache_weigh(const WeighArgs &a, int dtype, hipStream_t s) {
@@ -422,7 +459,7 @@ int launch_cache_weigh(const WeighArgs &a, int dtype, hipStream_t s) {
     p.rows = a.tokens * a.group;
     p.tiles = (int32_t)ceil_div(p.rows, 16);
     p.scale2 = a.scale * kLog2e;
-    p.units = (int64_t)a.c.batch * a.c.heads * ceil_div(a.c.capacity, 64);
+    p.units = (int64_t)a.c.batch * a.c.heads * ceil_div(a.c.capacity, 64 * kWeighGroups);
     return dtype == HBFP_F32 ? launch_weigh_of<HBFP_F32>(p, s) : dtype == HBFP_BF16 ? launch_weigh_of<HBFP_BF16>(p, s) : launch_weigh_of<HBFP_F16>(p, s);
 }
 

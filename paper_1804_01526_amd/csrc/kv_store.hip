@@ -165,9 +165,10 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const ReadParams p) {
     }
 }
 
-// ---- eviction.  One workgroup per head finds the keep - r largest of its first n - r weights: the smallest weight that stays
-// is found eight bits at a time from counts of the values that share the bits above (integers in the order of the weights),
-// then one ordered walk writes the slots that stay.  The order of the counts' additions does not change them.
+// ---- eviction.  One workgroup per head finds the keep - r largest of its first n - r weights: the smallest weight that stays is
+// found 11, 11 and 10 bits at a time from counts of the values that share the bits above (integers in the order of the weights;
+// eleven bits, because a histogram of exponents alone has all lanes at the same few counters), then one ordered walk writes the
+// slots that stay.  A thread has 16 consecutive weights of a segment, in registers when one segment is all.
 struct EvictParams {
     CacheView src, dst;
     const float *w;
@@ -184,58 +185,97 @@ __device__ __forceinline__ uint32_t ordered(float x) {
     const uint32_t u = __float_as_uint(x + 0.0f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-constexpr int kSelectThreads = 1024;
+constexpr int kOwn = 16, kBins = 2048;
 
-__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const EvictParams p) {
-    __shared__ uint32_t count[256];
-    __shared__ uint32_t sums[2][kSelectThreads / 64];
+// exclusive sums over the workgroup's threads, and the total; `sums`: one word per wave
+template <int THREADS>
+__device__ __forceinline__ uint32_t block_before(uint32_t x, uint32_t *sums, uint32_t &total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t upto = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t y = __shfl_up(upto, o);
+        if (lane >= o) upto += y;
+    }
+    __syncthreads();                                         // (the words of the call before have been read)
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    uint32_t before = upto - x;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        const uint32_t s = sums[w];
+        before += w < wave ? s : 0u;
+        total += s;
+    }
+    return before;
+}
+
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictParams p) {
+    constexpr int kSegment = THREADS * kOwn, PER = kBins / THREADS;
+    __shared__ uint32_t count[kBins];
+    __shared__ uint32_t sums[THREADS / 64];
     __shared__ uint32_t found[2];
     const int64_t bh = blockIdx.x;
-    const int b = (int)(bh / p.src.heads), t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int b = (int)(bh / p.src.heads), t = threadIdx.x;
     const int n = clamp_length(p.lengths[b], p.src.capacity);
     const int m = n < p.keep ? n : p.keep;
     const float *w = p.w + bh * p.ld;
     float *w_out = p.w_out + bh * p.ld_out;
     int32_t *kept = p.kept + bh * p.keep;
     if (t == 0 && bh % p.src.heads == 0) p.lengths_out[b] = m;
-    for (int i = m + t; i < p.keep; i += kSelectThreads) kept[i] = -1;
-    for (int i = m + t; i < p.dst.capacity; i += kSelectThreads) w_out[i] = 0.0f;
+    for (int i = m + t; i < p.keep; i += THREADS) kept[i] = -1;
+    for (int i = m + t; i < p.dst.capacity; i += THREADS) w_out[i] = 0.0f;
     if (n <= p.keep) {
-        for (int i = t; i < n; i += kSelectThreads) kept[i] = i, w_out[i] = w[i];
+        for (int i = t; i < n; i += THREADS) kept[i] = i, w_out[i] = w[i];
         return;
     }
     const int r = p.recent < p.keep ? p.recent : p.keep, others = n - r, top = p.keep - r;
+    float own[kOwn];
+    const auto load = [&](int segment) {
+        const int i0 = segment * kSegment + t * kOwn;
+#pragma unroll
+        for (int i = 0; i < kOwn; i += 4) {
+            if (i0 + i + 4 <= n) {
+                const v4f_at x = *reinterpret_cast<const v4f_at *>(w + i0 + i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) own[i + k] = x[k];
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) own[i + k] = i0 + i + k < n ? w[i0 + i + k] : 0.0f;
+            }
+        }
+    };
+    const int segments = (n + kSegment - 1) / kSegment;
+    if (segments == 1) load(0);
     // the top-th largest of w[0 .. others): its bits in `prefix`, how many equal ones stay in `ties`
     uint32_t prefix = 0, ties = (uint32_t)top;
     if (top > 0) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (t < 256) count[t] = 0;
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+            const uint32_t digit = pass == 2 ? 1023u : 2047u, above = pass == 0 ? 0u : pass == 1 ? ~0u << 21 : ~0u << 10;
+            for (int i = t; i < kBins; i += THREADS) count[i] = 0;
             __syncthreads();
-            const uint32_t above = shift == 24 ? 0u : ~0u << (shift + 8);
-            for (int i = t; i < others; i += kSelectThreads) {
-                const uint32_t key = ordered(w[i]);
-                if ((key & above) == prefix) atomicAdd(&count[(key >> shift) & 255u], 1u);
+            for (int segment = 0; segment < segments; ++segment) {
+                if (segments > 1) load(segment);
+                const int i0 = segment * kSegment + t * kOwn;
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) {
+                    const uint32_t key = ordered(own[i]);
+                    if (i0 + i < others && (key & above) == prefix) atomicAdd(&count[(key >> shift) & digit], 1u);
+                }
             }
             __syncthreads();
-            if (wave == 0) {
-                // lane l: the four digits from 255 - 4 l down; how many keys have larger digits
-                uint32_t c[4], own = 0;
+            // thread t: PER digits from the largest, 2047, down; how many keys have larger ones
+            uint32_t c[PER], mine = 0, all;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) own += c[i] = count[255 - 4 * lane - i];
-                uint32_t upto = own;
-                for (int o = 1; o < 64; o <<= 1) {
-                    const uint32_t x = __shfl_up(upto, o);
-                    if (lane >= o) upto += x;
-                }
-                uint32_t before = upto - own;
+            for (int i = 0; i < PER; ++i) mine += c[i] = count[kBins - 1 - PER * t - i];
+            uint32_t before = block_before<THREADS>(mine, sums, all);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (before < ties && ties <= before + c[i]) {
-                        found[0] = 255 - 4 * lane - i;
-                        found[1] = ties - before;
-                    }
-                    before += c[i];
-                }
+            for (int i = 0; i < PER; ++i) {
+                if (before < ties && ties <= before + c[i]) found[0] = kBins - 1 - PER * t - i, found[1] = ties - before;
+                before += c[i];
             }
             __syncthreads();
             prefix |= found[0] << shift;
@@ -244,86 +284,88 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
     }
     // ordered walk: slot i stays if it is recent, above the bound, or one of the first `ties` at it
     uint32_t out = 0, equal_before = 0;
-    for (int i0 = 0; i0 < n; i0 += kSelectThreads) {
-        const int i = i0 + t;
-        float x = 0.0f;
-        bool above = false, equal = false;
-        if (i < n) {
-            x = w[i];
-            if (i >= others) above = true;
-            else if (top > 0) {
-                const uint32_t key = ordered(x);
-                above = key > prefix;
-                equal = key == prefix;
-            }
+    for (int segment = 0; segment < segments; ++segment) {
+        if (segments > 1) load(segment);
+        const int i0 = segment * kSegment + t * kOwn;
+        uint32_t stays = 0, equal = 0;                        // a bit for each own weight
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const uint32_t key = ordered(own[i]);
+            const bool here = i0 + i < n, late = i0 + i >= others;
+            if (here && (late || (top > 0 && key > prefix))) stays |= 1u << i;
+            else if (here && top > 0 && key == prefix) equal |= 1u << i;
         }
-        const uint64_t eq = __ballot(equal), below = ((uint64_t)1 << lane) - 1;
-        if (lane == 0) sums[0][wave] = (uint32_t)__popcll(eq);
-        __syncthreads();
-        uint32_t rank = equal_before + (uint32_t)__popcll(eq & below), all = 0;
-        for (int k = 0; k < kSelectThreads / 64; ++k) {
-            const uint32_t s = sums[0][k];
-            if (k < wave) rank += s;
-            all += s;
-        }
+        uint32_t all;
+        uint32_t rank = equal_before + block_before<THREADS>((uint32_t)__popc(equal), sums, all);
         equal_before += all;
-        const bool stays = above || (equal && rank < ties);
-        const uint64_t st = __ballot(stays);
-        if (lane == 0) sums[1][wave] = (uint32_t)__popcll(st);
-        __syncthreads();
-        uint32_t pos = out + (uint32_t)__popcll(st & below);
-        all = 0;
-        for (int k = 0; k < kSelectThreads / 64; ++k) {
-            const uint32_t s = sums[1][k];
-            if (k < wave) pos += s;
-            all += s;
-        }
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i)
+            if (equal >> i & 1u) {
+                if (rank < ties) stays |= 1u << i;
+                ++rank;
+            }
+        uint32_t pos = out + block_before<THREADS>((uint32_t)__popc(stays), sums, all);
         out += all;
-        if (stays) kept[pos] = i, w_out[pos] = x;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i)
+            if (stays >> i & 1u) {
+                kept[pos] = i0 + i;
+                w_out[pos] = own[i];
+                ++pos;
+            }
     }
 }
 
-// Copies the kept slots: a thread takes 16 bytes of a key row, or one word of a value group (a byte from each of four slots).
+// Copies the kept slots.  Sixteen lanes have a group of four: lane c copies a quarter of one of its key rows (c / 4, c % 4) and
+// joins column c of its values from the columns of the four slots' groups, whole words of which one byte is theirs.
+template <int NB>
 __global__ __launch_bounds__(256) void evict_copy_kernel(const EvictParams p) {
-    const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (unit >= p.units) return;
-    const int nblk = p.src.nblk, per = 21 * nblk;               // 4 * nblk key pieces, 16 * nblk value words, nblk words of exponents
-    const int groups = (p.keep + 3) >> 2;
-    const int piece = (int)(unit % per);
-    const int64_t gi = unit / per, bh = gi / groups;
+    const int64_t gi = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (gi >= p.units) return;
+    const int groups = (p.keep + 3) >> 2, c = threadIdx.x & 15;
+    const int64_t bh = gi / groups;
     const int group = (int)(gi % groups);
     const int32_t *kept = p.kept + bh * p.keep;
     int from[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) from[j] = 4 * group + j < p.keep ? kept[4 * group + j] : -1;
     if (from[0] < 0) return;
-    if (piece < 4 * nblk) {
-        const int j = piece / nblk, part = piece % nblk;
-        int f = from[0];
+    const uint8_t *sk = p.src.k + bh * p.src.head_codes, *sv = p.src.v + bh * p.src.head_codes;
+    const uint8_t *ske = p.src.ke + bh * p.src.head_exps, *sve = p.src.ve + bh * p.src.head_exps;
+    uint32_t kw[NB], vw[4][NB];
+    const int j = c >> 2;
+    int f = from[0];
 #pragma unroll
-        for (int i = 1; i < 4; ++i) f = j == i ? from[i] : f;
-        if (f < 0) return;
-        *reinterpret_cast<v4u *>(p.dst.k + bh * p.dst.head_codes + ((int64_t)(4 * group + j) * nblk + part) * 16) =
-            *reinterpret_cast<const v4u *>(p.src.k + bh * p.src.head_codes + ((int64_t)f * nblk + part) * 16);
-    } else if (piece < 20 * nblk) {
-        const int word = piece - 4 * nblk;
-        const uint8_t *v = p.src.v + bh * p.src.head_codes + word * 4;
+    for (int i = 1; i < 4; ++i) f = j == i ? from[i] : f;
+    if (f >= 0) load_words<NB>(sk + ((int64_t)f * 16 + (c & 3) * 4) * NB, kw);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int slot = from[i] < 0 ? from[0] : from[i];       // (no such slot: any that exists, nothing reads the result)
+        load_words<NB>(sv + ((int64_t)(slot >> 2) * 64 + c * 4) * NB, vw[i]);
+    }
+    if (f >= 0) {
+        uint32_t *const dst = reinterpret_cast<uint32_t *>(p.dst.k + bh * p.dst.head_codes + ((int64_t)(4 * group + j) * 16 + (c & 3) * 4) * NB);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) dst[i] = kw[i];
+    }
+    uint32_t *const dst = reinterpret_cast<uint32_t *>(p.dst.v + bh * p.dst.head_codes + ((int64_t)group * 64 + c * 4) * NB);
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
         uint32_t r = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (from[j] >= 0) r |= (uint32_t)v[(int64_t)(from[j] >> 2) * 64 * nblk + (from[j] & 3)] << (8 * j);
-        *reinterpret_cast<uint32_t *>(p.dst.v + bh * p.dst.head_codes + (int64_t)group * 64 * nblk + word * 4) = r;
-    } else {
-        const int blk = piece - 20 * nblk;
+        for (int i = 0; i < 4; ++i) r |= ((vw[i][blk] >> (8 * (from[i] & 3))) & 0xffu) << (8 * i);
+        dst[blk] = r;
+    }
+    if (c < NB) {
         uint32_t rk = 0, rv = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (from[j] >= 0) {
-                const int64_t e = bh * p.src.head_exps + ((int64_t)(from[j] >> 2) * nblk + blk) * 4 + (from[j] & 3);
-                rk |= (uint32_t)p.src.ke[e] << (8 * j);
-                rv |= (uint32_t)p.src.ve[e] << (8 * j);
+        for (int i = 0; i < 4; ++i)
+            if (from[i] >= 0) {
+                const int64_t e = ((int64_t)(from[i] >> 2) * NB + c) * 4 + (from[i] & 3);
+                rk |= (uint32_t)ske[e] << (8 * i);
+                rv |= (uint32_t)sve[e] << (8 * i);
             }
-        const int64_t e = bh * p.dst.head_exps + ((int64_t)group * nblk + blk) * 4;
+        const int64_t e = bh * p.dst.head_exps + ((int64_t)group * NB + c) * 4;
         *reinterpret_cast<uint32_t *>(p.dst.ke + e) = rk;
         *reinterpret_cast<uint32_t *>(p.dst.ve + e) = rv;
     }
@@ -364,11 +406,15 @@ int launch_cache_read(const CacheView &c, const int32_t *lengths, int dtype, voi
 int launch_cache_evict(const CacheView &src, const float *w, int64_t ld, const int32_t *lengths, int64_t keep, int64_t recent,
                        const CacheView &dst, float *w_out, int64_t ld_out, int32_t *kept, int32_t *lengths_out, hipStream_t s) {
     EvictParams p = {src, dst, w, w_out, lengths, kept, lengths_out, ld, ld_out, (int32_t)keep, (int32_t)recent, 0};
-    p.units = (int64_t)src.batch * src.heads * ceil_div(keep, 4) * 21 * src.nblk;
-    const int64_t wgs = ceil_div(p.units, 256);
+    p.units = (int64_t)src.batch * src.heads * ceil_div(keep, 4);
+    const int64_t wgs = ceil_div(p.units, 16);
+    static void (*const copies[8])(EvictParams) = {&evict_copy_kernel<1>, &evict_copy_kernel<2>, &evict_copy_kernel<3>, &evict_copy_kernel<4>,
+                                                   &evict_copy_kernel<5>, &evict_copy_kernel<6>, &evict_copy_kernel<7>, &evict_copy_kernel<8>};
     if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
-    hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)(src.batch * src.heads)), dim3(kSelectThreads), 0, s, p);
-    hipLaunchKernelGGL(evict_copy_kernel, dim3((unsigned)wgs), dim3(256), 0, s, p);
+    // a segment that holds the whole cache, if one does: four waves for small caches (barriers among 16 cost 600 slots 15 us)
+    if (src.capacity <= 256 * kOwn) hipLaunchKernelGGL(evict_select_kernel<256>, dim3((unsigned)(src.batch * src.heads)), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(evict_select_kernel<1024>, dim3((unsigned)(src.batch * src.heads)), dim3(1024), 0, s, p);
+    hipLaunchKernelGGL(copies[src.nblk - 1], dim3((unsigned)wgs), dim3(256), 0, s, p);
     return launch_status();
 }
 
