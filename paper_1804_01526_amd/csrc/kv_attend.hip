@@ -12,12 +12,12 @@
 namespace hbfp {
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4, kStepKeys = 32;
 
 // a wave's 16 queries as the second operand of S^T = K Q^T: lane c + 16 g has dimensions 32 blk + 8 g .. + 7 of query c
 template <int NB, int DT>
 __device__ __forceinline__ void load_queries(const Heads &q, int64_t b, int key_head, int group, int row, int rows, int dim, int g,
-                                             v8bf (&out)[Pieces<DT>::n][NB]) {
+                                             bool negate, v8bf (&out)[Pieces<DT>::n][NB]) {
     const bool real = row < rows;
     const int t = real ? row / group : 0, h = real ? key_head * group + row % group : 0;
     const int64_t base = b * q.sb + t * q.st + h * q.sh;
@@ -26,6 +26,9 @@ __device__ __forceinline__ void load_queries(const Heads &q, int64_t b, int key_
         const int d0 = 32 * blk + 8 * g, n = real ? dim - d0 : 0;
         float x[8];
         load8<DT>(q.data, base + d0, n, x);
+        if (negate)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = -x[i];
         uint32_t w[4][Pieces<DT>::n];
 #pragma unroll
         for (int i = 0; i < 4; ++i) bf16_pieces2<Pieces<DT>::n>(x[2 * i], x[2 * i + 1], w[i]);
@@ -50,24 +53,34 @@ __device__ __forceinline__ v4f scores16(const uint32_t (&w)[NB], const uint32_t 
     return s;
 }
 
+// The words of KS keys and values that a lane needs
+template <int NB, int KS>
+struct StepWords {
+    uint32_t kw[KS / 16][NB], kx[KS / 16][NB], vw[KS / 16][NB], vx[KS / 16][NB];
+};
+template <int NB, int KS>
+__device__ __forceinline__ void request_step(const uint8_t *k, const uint8_t *ke, const uint8_t *v, const uint8_t *ve, int key0, int c, int g,
+                                             StepWords<NB, KS> &r) {
+#pragma unroll
+    for (int t = 0; t < KS / 16; ++t) {
+        const uint32_t key = key0 + 16 * t + c, group = (key0 + 16 * t) / 4;
+        load_words<NB>(k + (key * 16 + g * 4) * NB, r.kw[t]);
+        load_words<NB>(ke + (group + c / 4) * 4 * NB, r.kx[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < KS / 16; ++t) {
+        const uint32_t group = (key0 + 16 * t) / 4 + g;
+        load_words<NB>(v + (group * 64 + c * 4) * NB, r.vw[t]);
+        load_words<NB>(ve + group * 4 * NB, r.vx[t]);
+    }
+}
+
 // One step of KS keys from key0 on.  MASK: some of the wave's queries do not see all of them.
 template <int NB, int NP, int KS, bool MASK>
-__device__ __forceinline__ void attend_step(const uint8_t *k, const uint8_t *ke, const uint8_t *v, const uint8_t *ve, int key0, int limit,
-                                            float scale2, int c, int g, const v8bf (&q)[NP][NB], v4f (&o)[2 * NB], float &m, float &l) {
+__device__ __forceinline__ void attend_step(const StepWords<NB, KS> &r, int key0, int limit, float scale2, int c, int g,
+                                            const v8bf (&q)[NP][NB], v4f (&o)[2 * NB], float &m, float &l) {
     constexpr int T = KS / 16;
-    uint32_t kw[T][NB], kx[T][NB], vw[T][NB], vx[T][NB];
-#pragma unroll
-    for (int t = 0; t < T; ++t) {
-        const uint32_t key = key0 + 16 * t + c, group = (key0 + 16 * t) / 4;
-        load_words<NB>(k + (key * 16 + g * 4) * NB, kw[t]);
-        load_words<NB>(ke + (group + c / 4) * 4 * NB, kx[t]);
-    }
-#pragma unroll
-    for (int t = 0; t < T; ++t) {
-        const uint32_t group = (key0 + 16 * t) / 4 + g;
-        load_words<NB>(v + (group * 64 + c * 4) * NB, vw[t]);
-        load_words<NB>(ve + group * 4 * NB, vx[t]);
-    }
+    const auto &kw = r.kw, &kx = r.kx, &vw = r.vw, &vx = r.vx;
     float s[T][4];
     float top = -INFINITY;
 #pragma unroll
@@ -75,25 +88,26 @@ __device__ __forceinline__ void attend_step(const uint8_t *k, const uint8_t *ke,
         const v4f x = scores16<NB, NP>(kw[t], kx[t], c & 3, q);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            s[t][i] = x[i] * scale2;
-            if (MASK) s[t][i] = key0 + 16 * t + 4 * g + i < limit ? s[t][i] : -INFINITY;
+            s[t][i] = MASK ? key0 + 16 * t + 4 * g + i < limit ? x[i] : -INFINITY : x[i];
             top = fmaxf(top, s[t][i]);
         }
     }
-    const float m_new = fmaxf(m, max_over_rows(top));
-    const float from = m_new == -INFINITY ? 0.0f : m_new;
-    if (__any(m_new > m)) {
-        const float shrink = __builtin_amdgcn_exp2f(m - from);
+    // m is the largest score up to a factor of 2^kSlack in its exponential: new largest scores are frequent among 16 queries, such
+    // that are that much larger are not after the first steps
+    top = max_over_rows(top) * scale2;
+    if (__any(top > m + kSlack)) {
+        const float m_new = fmaxf(m, top), shrink = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
         l *= shrink;
 #pragma unroll
         for (int i = 0; i < 2 * NB; ++i) o[i] *= shrink;
         m = m_new;
     }
+    const float from = m == -INFINITY ? 0.0f : m;
 #pragma unroll
     for (int t = 0; t < T; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            s[t][i] = __builtin_amdgcn_exp2f(s[t][i] - from);
+            s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], scale2, -from));
             l += s[t][i];
         }
 #pragma unroll
@@ -104,14 +118,9 @@ __device__ __forceinline__ void attend_step(const uint8_t *k, const uint8_t *ke,
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; i += 2) {
-                    float x = s[u + t][i] * exponent_scale(vx[u + t][blk], i), y = s[u + t][i + 1] * exponent_scale(vx[u + t][blk], i + 1);
-                    if (MASK) {                             // a weight of 0 stays 0 whatever the exponent byte
-                        x = s[u + t][i] == 0.0f ? 0.0f : x;
-                        y = s[u + t][i + 1] == 0.0f ? 0.0f : y;
-                    }
-                    bf16_pieces2<NP>(x, y, w[2 * t + i / 2]);
-                }
+                for (int i = 0; i < 4; i += 2)             // (a weight of 0 stays 0 whatever the exponent byte)
+                    bf16_pieces2<NP>(times_exponent(s[u + t][i], vx[u + t][blk], i), times_exponent(s[u + t][i + 1], vx[u + t][blk], i + 1),
+                                     w[2 * t + i / 2]);
             const uint32_t lo0 = fp8_of_low(vw[u][blk]), lo1 = fp8_of_low(vw[u + 1][blk]);
             const uint32_t hi0 = fp8_of_high(vw[u][blk]), hi1 = fp8_of_high(vw[u + 1][blk]);
             const v4u lo = {bf16_pair<false>(lo0, 1.0f), bf16_pair<true>(lo0, 1.0f), bf16_pair<false>(lo1, 1.0f), bf16_pair<true>(lo1, 1.0f)};
@@ -130,7 +139,7 @@ __device__ __forceinline__ void attend_step(const uint8_t *k, const uint8_t *ke,
 // ones go to the workspace, and cache_join_kernel joins those.
 template <int NB, int DT>
 __global__ __launch_bounds__(64 * kWaves, NB <= 4 ? 2 : 1) void cache_attend_kernel(const SplitParams p) {
-    constexpr int NP = Pieces<DT>::n, KS = NB <= 4 ? 64 : 32, DP = 32 * NB, PITCH = DP + 4;
+    constexpr int NP = Pieces<DT>::n, KS = kStepKeys, DP = 32 * NB, PITCH = DP + 4;
     extern __shared__ __attribute__((aligned(16))) float lds[];          // [wave][16 queries][PITCH], then [wave][16] max, [wave][16] sum
     const CacheView &cache = p.a.c;
     uint32_t id = blockIdx.x;
@@ -154,16 +163,30 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 4 ? 2 : 1) void cache_attend_ker
     const int row = 16 * tile + c;
     const int limit = row < p.rows ? visible(length, p.a.tokens, p.a.group, row, p.a.causal, bound) : 0;
     v8bf q[NP][NB];
-    load_queries<NB, DT>(p.a.q, b, key_head, p.a.group, row, p.rows, cache.dim, g, q);
+    load_queries<NB, DT>(p.a.q, b, key_head, p.a.group, row, p.rows, cache.dim, g, p.a.scale < 0.0f, q);   // (scale2 is the magnitude)
     const uint8_t *k = cache.k + bh * cache.head_codes, *v = cache.v + bh * cache.head_codes;
     const uint8_t *ke = cache.ke + bh * cache.head_exps, *ve = cache.ve + bh * cache.head_exps;
     v4f o[2 * NB];
 #pragma unroll
     for (int i = 0; i < 2 * NB; ++i) o[i] = v4f{0, 0, 0, 0};
     float m = -INFINITY, l = 0.0f;
-    for (int key0 = begin + wave * KS; key0 < end; key0 += kWaves * KS) {
-        if (key0 + KS <= least) attend_step<NB, NP, KS, false>(k, ke, v, ve, key0, limit, p.scale2, c, g, q, o, m, l);
-        else attend_step<NB, NP, KS, true>(k, ke, v, ve, key0, limit, p.scale2, c, g, q, o, m, l);
+    // a step's words are on their way while the step before it is computed
+    constexpr int STRIDE = kWaves * KS;
+    StepWords<NB, KS> r0, r1;
+    int key0 = begin + wave * KS;
+    const auto request = [&](int at, StepWords<NB, KS> &r) {
+        if (at < end) request_step<NB, KS>(k, ke, v, ve, at, c, g, r);
+    };
+    request(key0, r0);
+    for (; key0 + STRIDE < end && key0 + STRIDE + KS <= least; key0 += 2 * STRIDE) {
+        request(key0 + STRIDE, r1);
+        attend_step<NB, NP, KS, false>(r0, key0, limit, p.scale2, c, g, q, o, m, l);
+        request(key0 + 2 * STRIDE, r0);
+        attend_step<NB, NP, KS, false>(r1, key0 + STRIDE, limit, p.scale2, c, g, q, o, m, l);
+    }
+    for (; key0 < end; key0 += STRIDE) {
+        attend_step<NB, NP, KS, true>(r0, key0, limit, p.scale2, c, g, q, o, m, l);
+        request(key0 + STRIDE, r0);
     }
     l = sum_over_rows(l);
     float *const lds_m = lds + kWaves * 16 * PITCH, *const lds_l = lds_m + kWaves * 16;
@@ -278,10 +301,10 @@ SplitParams split_of(const AttendArgs &a, int dtype) {
     p.tile_rows = prompt ? (int32_t)cache_prompt_rows(a) : 16;
     p.tiles = (int32_t)ceil_div(p.rows, p.tile_rows);
     p.scale2 = a.scale * kLog2e;
-    if (prompt) p.scale2 = p.scale2 == 0.0f ? 1.2e-38f : p.scale2 < 0.0f ? -p.scale2 : p.scale2;     // (0 times a masked -infinity is no number)
+    p.scale2 = p.scale2 == 0.0f ? 1.2e-38f : p.scale2 < 0.0f ? -p.scale2 : p.scale2;     // (0 times a masked -infinity is no number)
     const int64_t heads = (int64_t)a.c.batch * a.c.heads * p.tiles;
-    const int64_t step = prompt ? 512 : kWaves * (a.c.nblk <= 4 ? 64 : 32);
-    const int64_t want = ceil_div(prompt ? 512 : 2048, heads);
+    const int64_t step = prompt ? 512 : kWaves * kStepKeys;
+    const int64_t want = ceil_div(prompt ? 512 : 1024, heads);
     p.chunk = (int32_t)round_up(ceil_div(a.longest, want), step);
     p.chunks = (int32_t)ceil_div(a.longest, p.chunk);
     return p;
@@ -365,7 +388,7 @@ __global__ __launch_bounds__(256) void cache_weigh_kernel(const WeighParams p) {
             limit = visible(length, p.a.tokens, p.a.group, row, p.a.causal, bound);
             lse2 = p.a.lse[(b * p.a.tokens + row / p.a.group) * p.a.heads + key_head * p.a.group + row % p.a.group] * kLog2e;
         }
-        load_queries<NB, DT>(p.a.q, b, key_head, p.a.group, row, p.rows, cache.dim, g, q);
+        load_queries<NB, DT>(p.a.q, b, key_head, p.a.group, row, p.rows, cache.dim, g, false, q);
     };
     uint32_t w[4][NB], e[4][NB];
     float before = 0.0f;

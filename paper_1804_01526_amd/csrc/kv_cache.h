@@ -15,6 +15,7 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
+constexpr float kSlack = 6.0f;             // of a running maximum, in powers of two
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // keys that row `row` (token row / group) of batch entry b may see
@@ -42,8 +43,10 @@ __device__ __forceinline__ uint32_t bf16_pair(uint32_t fp8, float scale) {
 }
 // the same scale for the FP8 conversion, which looks at nothing but the exponent field: the byte `j` of a word moved there
 __device__ __forceinline__ float conversion_scale(uint32_t word, int j) { return __uint_as_float(j < 3 ? word << (23 - 8 * j) : word >> 1); }
-// the 2^(Eb - 127) of the exponent byte `j` of a word
-__device__ __forceinline__ float exponent_scale(uint32_t word, int j) { return __uint_as_float(((word >> (8 * j)) & 0xffu) << 23); }
+// x times the 2^(Eb - 127) of the exponent byte `j` of a word; 0 stays 0 for every byte
+__device__ __forceinline__ float times_exponent(float x, uint32_t word, int j) {
+    return __builtin_amdgcn_ldexpf(x, (int)((word >> (8 * j)) & 0xffu) - 127);
+}
 
 // eight values in the order low nibbles, high nibbles (for the key layout: dimensions 8 g .. 8 g + 7)
 __device__ __forceinline__ v8bf key_values(uint32_t w, float scale) {

@@ -13,7 +13,6 @@ namespace {
 struct No { static constexpr bool value = false; };
 struct Yes { static constexpr bool value = true; };
 constexpr int kTile = 64;                  // keys
-constexpr float kSlack = 6.0f;
 constexpr int kValuePitch = kTile * 2 + 16;  // bytes of a row of transposed values: 16 more than its keys, so that rows differ in banks
 template <int NB> struct PromptLds {
     static constexpr int kKeyPitch = 64 * NB + 16, kKeys = kTile * kKeyPitch, kValues = 32 * NB * kValuePitch;
