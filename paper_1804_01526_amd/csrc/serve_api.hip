@@ -160,7 +160,7 @@ int hbfp_cache_attend(const hbfp_cache *cache, const hbfp_heads *q, int64_t toke
     a.lse = lse;
     a.causal = causal;
     a.scale = scale;
-    const size_t need = cache_attend_workspace(a, q->dtype);
+    const size_t need = align256(cache_attend_workspace(a, q->dtype));
     if (need && (!workspace || ws_bytes < need || ((uintptr_t)workspace & 255))) return HBFP_ERR_WORKSPACE;
     a.ws = need ? (float *)workspace : nullptr;
     return launch_cache_attend(a, q->dtype, (hipStream_t)stream);
@@ -245,7 +245,7 @@ int hbfp_gemm_rows(const int8_t *a, const float *a_scales, const int8_t *b, cons
     if (!a || !b || !a_scales || !b_scales || (((uintptr_t)a | (uintptr_t)b) & 15)) return HBFP_ERR_ARG;
     if (((uintptr_t)a_scales | (uintptr_t)b_scales | (uintptr_t)bias) & 3) return HBFP_ERR_ARG;
     if ((rc = check_matrix(y, dtype, M, N, ldy)) != HBFP_OK) return rc;
-    const size_t need = gemm_rows_workspace(M, N, round_up(K, 128));
+    const size_t need = align256(gemm_rows_workspace(M, N, round_up(K, 128)));
     if (need && (!workspace || ws_bytes < need || ((uintptr_t)workspace & 255))) return HBFP_ERR_WORKSPACE;
     const RowsArgs r = {a, b, a_scales, b_scales, bias, y, M, N, K, round_up(K, 128), ldy, dtype};
     return launch_gemm_rows(r, workspace, (hipStream_t)stream);
