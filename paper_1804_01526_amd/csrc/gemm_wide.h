@@ -113,7 +113,7 @@ __device__ __forceinline__ void store_result16(uint16_t *dst, int64_t ld, int64_
 }
 
 // STREAM: how C leaves (stores_stream)
-template <int T, int K, int RING, bool STREAM, int OUT>
+template <int T, int K, int RING, int OUT, bool STREAM>
 __global__ __launch_bounds__(kWideThreads, T == 4 ? 1 : 2) void gemm_i8_wide_kernel(const WideParams p) {
     typedef Wide<T, K, RING> W;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(kWideThreads, T == 4 ? 1 : 2) void gemm_i8_wide_ker
 // The sum of the slices of a product split along k: int32, so any order gives the same bits, those of the unsplit product.
 // A thread sums four outputs 256 apart, eight slices in flight each.
 template <int OUT>
-__global__ __launch_bounds__(256) void wide_sum_kernel(const WideParams p) {
+__device__ __forceinline__ void wide_sum(const WideParams &p) {
     if (stands_down(p.run_a, p.run_b)) return;
     const int64_t n = p.M * p.N;
     const int64_t e0 = (int64_t)blockIdx.x * 1024 + threadIdx.x;
@@ -370,12 +370,15 @@ __global__ __launch_bounds__(256) void wide_sum_kernel(const WideParams p) {
         *dst = p.beta ? *dst + val : val;
     }
 }
+__global__ __launch_bounds__(256) void wide_sum_kernel(const WideParams p) { wide_sum<kWideExponents>(p); }
+template <int OUT>
+__global__ __launch_bounds__(256) void rows_sum_kernel(const WideParams p) { wide_sum<OUT>(p); }
 
 template <int T, int K, int RING, int OUT>
 int launch_wide_t(WideParams p, bool stream, hipStream_t s) {
     static std::atomic<bool> configured[2];
     constexpr int lds_bytes = Wide<T, K, RING>::kLds;
-    void (*const kernel)(WideParams) = stream ? &gemm_i8_wide_kernel<T, K, RING, true, OUT> : &gemm_i8_wide_kernel<T, K, RING, false, OUT>;
+    void (*const kernel)(WideParams) = stream ? &gemm_i8_wide_kernel<T, K, RING, OUT, true> : &gemm_i8_wide_kernel<T, K, RING, OUT, false>;
     if (allow_dynamic_lds(configured[stream], reinterpret_cast<const void *>(kernel), lds_bytes) != HBFP_OK) return HBFP_ERR_LAUNCH;
     p.nstage *= 128 / K;
     p.stages_per_split *= 128 / K;
@@ -451,7 +454,8 @@ int launch_wide_planned(WideParams p, const WidePlan &plan, bool stream, hipStre
     if (rc != HBFP_OK || p.splits == 1) return rc;
     const int64_t wgs = ceil_div(p.M * p.N, 1024);
     if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
-    hipLaunchKernelGGL(wide_sum_kernel<OUT>, dim3((unsigned)wgs), dim3(256), 0, s, p);
+    if constexpr (OUT == kWideExponents) hipLaunchKernelGGL(wide_sum_kernel, dim3((unsigned)wgs), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(rows_sum_kernel<OUT>, dim3((unsigned)wgs), dim3(256), 0, s, p);
     return launch_status();
 }
 
