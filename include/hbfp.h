@@ -758,8 +758,8 @@ int hbfp_cache_read(const hbfp_cache *cache, const int32_t *lengths, int dtype, 
  *   lse  [batch][tokens][heads] FP32: log(sum exp(s)) over the visible keys;  out = sum exp(s - lse) v
  *   A query that sees no key: out = 0, lse = -infinity.  Masked keys and values have no influence, whatever they hold.
  *   longest  the caller's bound on the lengths (it sizes the launch); 0 = the capacity.  Keys from it on are not seen.
- * The scores, the softmax statistics and the sums are FP32.  bf16 queries enter the products exactly and the weights exp(s - max)
- * rounded to bf16; FP16 queries exactly and the weights as two bf16 numbers (16 bits); FP32 both as three (24 bits).
+ * The scores, the softmax statistics and the sums are FP32.  bf16 and FP16 queries enter the products exactly and the weights
+ * exp(s - max) as two bf16 numbers (16 bits); FP32 both as three (24 bits).
  * workspace: hbfp_cache_attend_workspace bytes, 256-byte aligned.  Errors: as hbfp_cache_append, HBFP_ERR_WORKSPACE.
  */
 int hbfp_cache_attend_workspace(const hbfp_cache *cache, int64_t tokens, int64_t heads, int dtype, int64_t longest, size_t *bytes);

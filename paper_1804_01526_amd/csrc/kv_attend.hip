@@ -76,7 +76,7 @@ __device__ __forceinline__ void request_step(const uint8_t *k, const uint8_t *ke
 }
 
 // One step of KS keys from key0 on.  MASK: some of the wave's queries do not see all of them.
-template <int NB, int NP, int KS, bool MASK>
+template <int NB, int NP, int NW, int KS, bool MASK>
 __device__ __forceinline__ void attend_step(const StepWords<NB, KS> &r, int key0, int limit, float scale2, int c, int g,
                                             const v8bf (&q)[NP][NB], v4f (&o)[2 * NB], float &m, float &l) {
     constexpr int T = KS / 16;
@@ -114,19 +114,19 @@ __device__ __forceinline__ void attend_step(const StepWords<NB, KS> &r, int key0
     for (int u = 0; u < T; u += 2)
 #pragma unroll
         for (int blk = 0; blk < NB; ++blk) {
-            uint32_t w[4][NP];
+            uint32_t w[4][NW];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; i += 2)             // (a weight of 0 stays 0 whatever the exponent byte)
-                    bf16_pieces2<NP>(times_exponent(s[u + t][i], vx[u + t][blk], i), times_exponent(s[u + t][i + 1], vx[u + t][blk], i + 1),
+                    bf16_pieces2<NW>(times_exponent(s[u + t][i], vx[u + t][blk], i), times_exponent(s[u + t][i + 1], vx[u + t][blk], i + 1),
                                      w[2 * t + i / 2]);
             const uint32_t lo0 = fp8_of_low(vw[u][blk]), lo1 = fp8_of_low(vw[u + 1][blk]);
             const uint32_t hi0 = fp8_of_high(vw[u][blk]), hi1 = fp8_of_high(vw[u + 1][blk]);
             const v4u lo = {bf16_pair<false>(lo0, 1.0f), bf16_pair<true>(lo0, 1.0f), bf16_pair<false>(lo1, 1.0f), bf16_pair<true>(lo1, 1.0f)};
             const v4u hi = {bf16_pair<false>(hi0, 1.0f), bf16_pair<true>(hi0, 1.0f), bf16_pair<false>(hi1, 1.0f), bf16_pair<true>(hi1, 1.0f)};
 #pragma unroll
-            for (int p = NP - 1; p >= 0; --p) {
+            for (int p = NW - 1; p >= 0; --p) {
                 const v4u pw = {w[0][p], w[1][p], w[2][p], w[3][p]};
                 const v8bf pb = __builtin_bit_cast(v8bf, pw);
                 o[2 * blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, lo), pb, o[2 * blk], 0, 0, 0);
@@ -137,12 +137,12 @@ __device__ __forceinline__ void attend_step(const StepWords<NB, KS> &r, int key0
 
 // Bound by bytes on their way and by the vector instructions that turn nibbles into numbers: with four queries a head only a quarter of
 // every tile of 16 is real, and the conversion is the same as for all.  16 heads (4 of keys) of 128 over 200001 tokens: 109 MB in
-// 36 us, 3.0 TB/s; 32 conversations of 128 to 8192 tokens, 32 heads (8 of keys): 62 MB in 27 us, 2.3 TB/s.
+// 37 us, 3.0 TB/s; 32 conversations of 128 to 8192 tokens, 32 heads (8 of keys): 62 MB in 30 us, 2.1 TB/s (weights as one piece: 27).
 // A workgroup's four waves take the steps of a chunk in turn and join their results in LDS; with several chunks the joined
 // ones go to the workspace, and cache_join_kernel joins those.
 template <int NB, int DT>
 __global__ __launch_bounds__(64 * kWaves, NB <= 4 ? 2 : 1) void cache_attend_kernel(const SplitParams p) {
-    constexpr int NP = Pieces<DT>::n, KS = kStepKeys, DP = 32 * NB, PITCH = DP + 4;
+    constexpr int NP = Pieces<DT>::n, NW = Pieces<DT>::weights, KS = kStepKeys, DP = 32 * NB, PITCH = DP + 4;
     extern __shared__ __attribute__((aligned(16))) float lds[];          // [wave][16 queries][PITCH], then [wave][16] max, [wave][16] sum
     const CacheView &cache = p.a.c;
     uint32_t id = blockIdx.x;
@@ -183,12 +183,12 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 4 ? 2 : 1) void cache_attend_ker
     request(key0, r0);
     for (; key0 + STRIDE < end && key0 + STRIDE + KS <= least; key0 += 2 * STRIDE) {
         request(key0 + STRIDE, r1);
-        attend_step<NB, NP, KS, false>(r0, key0, limit, p.scale2, c, g, q, o, m, l);
+        attend_step<NB, NP, NW, KS, false>(r0, key0, limit, p.scale2, c, g, q, o, m, l);
         request(key0 + 2 * STRIDE, r0);
-        attend_step<NB, NP, KS, false>(r1, key0 + STRIDE, limit, p.scale2, c, g, q, o, m, l);
+        attend_step<NB, NP, NW, KS, false>(r1, key0 + STRIDE, limit, p.scale2, c, g, q, o, m, l);
     }
     for (; key0 < end; key0 += STRIDE) {
-        attend_step<NB, NP, KS, true>(r0, key0, limit, p.scale2, c, g, q, o, m, l);
+        attend_step<NB, NP, NW, KS, true>(r0, key0, limit, p.scale2, c, g, q, o, m, l);
         request(key0 + STRIDE, r0);
     }
     l = sum_over_rows(l);

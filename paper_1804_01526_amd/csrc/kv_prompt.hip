@@ -4,9 +4,10 @@
 // values are turned into bf16 numbers once, exactly, by all its waves together, into LDS: keys as they are, values transposed,
 // in the order in which the scores' register layout presents keys.  Then S^T = K Q^T and O^T += V^T P^T as in the kernel for
 // few queries, on the 32 x 32 x 16 matrix instruction: a lane holds one query, and its softmax needs one exchange with the lane
-// 32 away.  Bound by the vector unit (exponentials, conversions, packing of weights) beside the matrix core: two prompts of 2048 tokens
-// over 4096, 32 heads (8 of keys) of 128, causal: 206 Gflop in 222 to 237 us, 0.9 PFLOP/s, three quarters of what a large bf16 product
-// reaches; three of 501 tokens, 6 heads (2 of keys) of 96, FP16 with two pieces a weight: 22 us and 4.8 for joining the chunks.
+// 32 away.  Weights enter the second product as two pieces (bf16, FP16), so it costs twice its operations.  Two prompts of 2048 tokens
+// over 4096, 32 heads (8 of keys) of 128, causal, bf16: 206 Gflop, 309 on the matrix core, in 296 us (one piece: 246), 1.04 PFLOP/s
+// of the 1.2 that a large bf16 product reaches; three of 501 tokens, 6 heads (2 of keys) of 96, FP16: 22 us and 4.7 for joining the
+// chunks.
 #include "kv_cache.h"
 
 namespace hbfp {
@@ -45,7 +46,7 @@ __device__ __forceinline__ void prompt_walk(const SplitParams &p, uint8_t *lds, 
                                             const uint8_t *ve, const v8bf (&q)[Pieces<DT>::n][2 * NB], int wave, int lane, int begin, int end,
                                             int wave_least, int wave_most, int limit, int stored_end, v16f (&o)[NB], float &m, float &l) {
     typedef PromptLds<NB> L;
-    constexpr int NP = Pieces<DT>::n;
+    constexpr int NP = Pieces<DT>::n, NW = Pieces<DT>::weights;
     constexpr int KI = BRINGS & kBringKeys ? (W == 8 ? 1 : 4 / W) : 0, VI = BRINGS & kBringValues ? (W == 8 ? 1 : 4 / W) : 0;
     const int l32 = lane & 31, h = lane >> 5;
     RawItem<NB> rk[KI ? KI : 1], rv[VI ? VI : 1];
@@ -139,8 +140,7 @@ __device__ __forceinline__ void prompt_walk(const SplitParams &p, uint8_t *lds, 
             m = m_new;
         }
     };
-    // the weights of a tile's scores; one piece: as the second operands of the products with the values, several: still in FP32
-    uint32_t packed[2][2][4];
+    // the weights of a tile's scores
     const auto weights = [&](v16f (&s)[2]) {
         const float from = m == -INFINITY ? 0.0f : m;
         float sum[2] = {0.0f, 0.0f};
@@ -152,7 +152,6 @@ __device__ __forceinline__ void prompt_walk(const SplitParams &p, uint8_t *lds, 
                 s[kt][x + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][x + 1], p.scale2, -from));
                 sum[0] += s[kt][x];
                 sum[1] += s[kt][x + 1];
-                if (NP == 1) packed[kt][x >> 3][(x >> 1) & 3] = bf16_bits2(s[kt][x], s[kt][x + 1]);
             }
         l += sum[0] + sum[1];
     };
@@ -162,17 +161,14 @@ __device__ __forceinline__ void prompt_walk(const SplitParams &p, uint8_t *lds, 
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                uint32_t w[4][NP];
+                uint32_t w[4][NW];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (NP == 1) w[i][0] = packed[kt][ks][i];
-                    else bf16_pieces2<NP>(s[kt][8 * ks + 2 * i], s[kt][8 * ks + 2 * i + 1], w[i]);
-                }
+                for (int i = 0; i < 4; ++i) bf16_pieces2<NW>(s[kt][8 * ks + 2 * i], s[kt][8 * ks + 2 * i + 1], w[i]);
 #pragma unroll
                 for (int i = 0; i < NB; ++i) {
                     const v8bf a = *reinterpret_cast<const v8bf *>(vb + 32 * i * kValuePitch + (32 * kt + 16 * ks) * 2);
 #pragma unroll
-                    for (int n = NP - 1; n >= 0; --n) {
+                    for (int n = NW - 1; n >= 0; --n) {
                         const v4u pw = {w[0][n], w[1][n], w[2][n], w[3][n]};
                         o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(v8bf, pw), o[i], 0, 0, 0);
                     }

@@ -1,0 +1,114 @@
+"""The serving operators' kernels at sizes that reach each of them, against 64 bits on the GPU.
+
+Attention is compared on the values that the cache holds (hbfp_cache_read, itself held to the definition in test_gpu_serve.py).
+Tolerances.  With u the unit roundoff of the output's type, w that of the softmax weights as the products take them (2^-16 for bf16
+and FP16: two pieces of 8 bits; 2^-24 for FP32) and d the relative error of an exponential,
+    d = (dim + 16) 2^-24 max|scale q k| + (64 + keys / 32) 2^-24,
+a sum before its rounding is off by e = (w + 2 d) sum p |v|, and an output by e + u (|out| + e); lse by d + 2^-22 (1 + |lse|)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+U = {F32: 2.0 ** -24, BF16: 2.0 ** -8, F16: 2.0 ** -11}
+U_WEIGHT = {F32: 2.0 ** -24, BF16: 2.0 ** -16, F16: 2.0 ** -16}
+
+
+@pytest.fixture(scope="module")
+def hb():
+    from paper_1804_01526_amd import hbfp
+    assert torch.cuda.is_available(), "these tests need the GPU"
+    return hbfp
+
+
+def _lens(lengths):
+    return torch.tensor(lengths, dtype=torch.int32, device="cuda")
+
+
+def _randn(gen, shape, dtype=F32, spread=1):
+    x = torch.randn(shape, generator=gen, device="cuda")
+    return (x * torch.exp2(torch.randint(-spread, spread + 1, shape, generator=gen, device="cuda").float())).to(dtype)
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _filled(hb, gen, batch, heads, capacity, dim, lengths):
+    """A cache of `lengths` tokens a batch entry in poisoned buffers, and the FP64 keys and values it holds."""
+    cache = hb.cache_alloc(batch, heads, capacity, dim)
+    for t in (cache.k, cache.v, cache.k_exps, cache.v_exps):
+        t.fill_(255)
+    if max(lengths) > 0:
+        k, v = (_randn(gen, (batch, max(lengths), heads, dim)) for _ in range(2))
+        hb.cache_append(cache, k, v, _lens(lengths))
+    k, v = hb.cache_read(cache, _lens(lengths))
+    return cache, k.double(), v.double()
+
+
+def _attend64(k, v, q, lengths, scale, causal=True, longest=None):
+    """(out, lse, spread, noise) in 64 bits: spread = sum p |v|, noise = the largest sum of |scale q k| of a visible key; and the
+    weights that each key of each key head received, [batch][key head][slot]."""
+    batch, tokens, heads, dim = q.shape
+    kv, capacity = k.shape[1], k.shape[2]
+    group = heads // kv
+    out, spread = (torch.zeros(q.shape, dtype=torch.float64, device="cuda") for _ in range(2))
+    lse = torch.full((batch, tokens, heads), -math.inf, dtype=torch.float64, device="cuda")
+    noise = torch.zeros((batch, tokens, heads), dtype=torch.float64, device="cuda")
+    got = torch.zeros((batch, kv, capacity), dtype=torch.float64, device="cuda")
+    at, t = torch.arange(capacity, device="cuda"), torch.arange(tokens, device="cuda").unsqueeze(1)
+    for b, n in enumerate(lengths):
+        bound = min(longest or capacity, capacity)
+        seen = torch.clamp(n - tokens + t + 1 if causal else torch.full_like(t, n), max=bound)
+        hidden = (at >= seen).repeat_interleave(group, dim=0)                    # rows: token, head of the group
+        for h in range(kv):
+            rows = q[b, :, h * group:(h + 1) * group].double().reshape(tokens * group, dim)
+            kt = k[b, h].t().contiguous()
+            s = (scale * (rows @ kt)).masked_fill(hidden, -math.inf)
+            top = s.amax(dim=1, keepdim=True)
+            w = torch.exp(s - torch.where(torch.isinf(top), torch.zeros_like(top), top))
+            total = w.sum(dim=1, keepdim=True)
+            p = w / torch.where(total == 0, torch.ones_like(total), total)
+            put = lambda dst, x: dst[b, :, h * group:(h + 1) * group].copy_(x.reshape(tokens, group, *x.shape[1:]))
+            put(out, p @ v[b, h])
+            put(spread, p @ v[b, h].abs())
+            put(lse, torch.log(total[:, 0]) + torch.where(torch.isinf(top), torch.zeros_like(top), top)[:, 0])
+            put(noise, ((scale * rows).abs() @ kt.abs()).masked_fill(hidden, 0).amax(dim=1))
+            got[b, h] = p.sum(dim=0)
+    return out, lse, spread, noise, got
+
+
+def _check_attend(got, got_lse, want, dtype, dim, keys):
+    out, lse, spread, noise, _ = want
+    d = (dim + 16) * 2.0 ** -24 * noise + (64 + keys / 32) * 2.0 ** -24
+    e = (U_WEIGHT[dtype] + 2 * d.unsqueeze(-1)) * spread
+    tol = e + U[dtype] * (out.abs() + e) + (2.0 ** -25 if dtype == F16 else 2.0 ** -140)
+    assert torch.isfinite(got).all()
+    ratio = ((got.double() - out).abs() / tol).max().item()
+    assert ratio <= 1, f"out: {ratio:.3f} of the tolerance"
+    empty = torch.isneginf(lse)
+    assert torch.equal(torch.isneginf(got_lse), empty) and (got[empty] == 0).all()
+    ratio = ((got_lse.double() - lse).abs() / (d + 2.0 ** -22 * (1 + lse.abs())))[~empty].max().item()
+    assert ratio <= 1, f"lse: {ratio:.3f} of the tolerance"
+
+
+# ------------------------------------------------------------------------------------------------------------- attention
+@pytest.mark.parametrize("batch,tokens,kv,group,dim,capacity,lengths", [
+    (2, 1, 2, 4, 64, 100, [100, 37]),                # one chunk of keys
+    (1, 1, 2, 8, 128, 5000, [4999]),                 # several
+    (2, 3, 1, 4, 256, 700, [700, 300]),
+    (1, 100, 2, 2, 128, 300, [300]),                 # a prompt
+    (2, 70, 1, 3, 72, 900, [900, 100]),
+])
+def test_bf16_outputs_lose_their_own_rounding_only(hb, batch, tokens, kv, group, dim, capacity, lengths):
+    """Softmax weights of bf16 calls enter the products with 16 bits."""
+    print(f"[attend] bf16 b{batch} t{tokens} h{kv}x{group} dim {dim} lengths {lengths}", flush=True)
+    gen = _gen(dim + tokens)
+    cache, k, v = _filled(hb, gen, batch, kv, capacity, dim, lengths)
+    q = _randn(gen, (batch, tokens, kv * group, dim), BF16)
+    out, lse = hb.cache_attend(cache, q, _lens(lengths))
+    _check_attend(out, lse, _attend64(k, v, q, lengths, dim ** -0.5), BF16, dim, capacity)
