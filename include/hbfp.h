@@ -759,7 +759,8 @@ int hbfp_cache_read(const hbfp_cache *cache, const int32_t *lengths, int dtype, 
  *   A query that sees no key: out = 0, lse = -infinity.  Masked keys and values have no influence, whatever they hold.
  *   longest  the caller's bound on the lengths (it sizes the launch); 0 = the capacity.  Keys from it on are not seen.
  * The scores, the softmax statistics and the sums are FP32.  bf16 and FP16 queries enter the products exactly and the weights
- * exp(s - max) as two bf16 numbers (16 bits); FP32 both as three (24 bits).
+ * exp(s - max) as two bf16 numbers (16 bits); FP32 both as three (24 bits).  Values of every magnitude below 2^127 have finite
+ * sums; what values below about 2^-70 contribute is off by 2^-90 at most.
  * workspace: hbfp_cache_attend_workspace bytes, 256-byte aligned.  Errors: as hbfp_cache_append, HBFP_ERR_WORKSPACE.
  */
 int hbfp_cache_attend_workspace(const hbfp_cache *cache, int64_t tokens, int64_t heads, int dtype, int64_t longest, size_t *bytes);

@@ -219,7 +219,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 4 ? 2 : 1) void cache_attend_ker
             if (d == 0) p.ml[2 * slot] = top, p.ml[2 * slot + 1] = sum;
         } else {
             const int tok = grow / p.a.group, h = key_head * p.a.group + grow % p.a.group;
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const float inv = sum == 0.0f ? 0.0f : kUp / sum;
             const float out4[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
             store4<DT>(p.a.out.data, b * p.a.out.sb + tok * p.a.out.st + h * p.a.out.sh + d, cache.dim - d, out4);
             if (d == 0) p.a.lse[(b * p.a.tokens + tok) * p.a.heads + h] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(THREADS) void cache_join_kernel(const SplitParams p
     }
     if (!real) return;
     const int tok = row / p.a.group, h = key_head * p.a.group + row % p.a.group;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float inv = l == 0.0f ? 0.0f : kUp / l;
     const float r[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
     store4<DT>(p.a.out.data, b * p.a.out.sb + tok * p.a.out.st + h * p.a.out.sh + d, cache.dim - d, r);
     if (d == 0) p.a.lse[(b * p.a.tokens + tok) * p.a.heads + h] = l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;

@@ -16,6 +16,10 @@ typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
 constexpr float kSlack = 6.0f;             // of a running maximum, in powers of two
+// Values enter the sums 2^-kDown times as large: weights of up to 2^kSlack times values below 2^127, over as many tokens as a head's buffer
+// can hold (2^27), stay below 2^128, and the division by the sum of the weights takes the factor back
+constexpr int kDown = 34;
+constexpr float kUp = 0x1p34f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // keys that row `row` (token row / group) of batch entry b may see
@@ -43,9 +47,13 @@ __device__ __forceinline__ uint32_t bf16_pair(uint32_t fp8, float scale) {
 }
 // the same scale for the FP8 conversion, which looks at nothing but the exponent field: the byte `j` of a word moved there
 __device__ __forceinline__ float conversion_scale(uint32_t word, int j) { return __uint_as_float(j < 3 ? word << (23 - 8 * j) : word >> 1); }
-// x times the 2^(Eb - 127) of the exponent byte `j` of a word; 0 stays 0 for every byte
+// ... of a block of values, 2^-kDown times as large (units below 2^-95 count as that: exponents end at 0)
+__device__ __forceinline__ float value_scale(uint32_t word, int j) {
+    return conversion_scale(word, j) * (1.0f / kUp);
+}
+// x times the 2^(Eb - 127 - kDown) of the exponent byte `j` of a word; 0 stays 0 for every byte
 __device__ __forceinline__ float times_exponent(float x, uint32_t word, int j) {
-    return __builtin_amdgcn_ldexpf(x, (int)((word >> (8 * j)) & 0xffu) - 127);
+    return __builtin_amdgcn_ldexpf(x, (int)((word >> (8 * j)) & 0xffu) - (127 + kDown));
 }
 
 // eight values in the order low nibbles, high nibbles (for the key layout: dimensions 8 g .. 8 g + 7)

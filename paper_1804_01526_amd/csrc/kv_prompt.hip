@@ -91,7 +91,7 @@ __device__ __forceinline__ void prompt_walk(const SplitParams &p, uint8_t *lds, 
 #pragma unroll
             for (int blk = 0; blk < NB; ++blk) {
                 const uint32_t x = rv[i].e[blk] & mask, lo = fp8_of_low(rv[i].w[blk]), hi = fp8_of_high(rv[i].w[blk]);
-                const float s0 = conversion_scale(x, 0), s1 = conversion_scale(x, 1), s2 = conversion_scale(x, 2), s3 = conversion_scale(x, 3);
+                const float s0 = value_scale(x, 0), s1 = value_scale(x, 1), s2 = value_scale(x, 2), s3 = value_scale(x, 3);
                 const v2u a = {bf16_pair2<false>(lo, s0, s1), bf16_pair2<true>(lo, s2, s3)};
                 const v2u z = {bf16_pair2<false>(hi, s0, s1), bf16_pair2<true>(hi, s2, s3)};
                 *reinterpret_cast<v2u *>(dst + 32 * blk * kValuePitch) = a;
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(64 * W, 2) void cache_prompt_kernel(const SplitPara
         return;
     }
     const int tok = row / p.a.group, head = key_head * p.a.group + row % p.a.group;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float inv = l == 0.0f ? 0.0f : kUp / l;
     const int64_t dst = b * p.a.out.sb + tok * p.a.out.st + head * p.a.out.sh;
 #pragma unroll
     for (int i = 0; i < NB; ++i)

@@ -38,14 +38,14 @@ def _gen(seed):
     return torch.Generator(device="cuda").manual_seed(seed)
 
 
-def _filled(hb, gen, batch, heads, capacity, dim, lengths):
+def _filled(hb, gen, batch, heads, capacity, dim, lengths, values=lambda v: v):
     """A cache of `lengths` tokens a batch entry in poisoned buffers, and the FP64 keys and values it holds."""
     cache = hb.cache_alloc(batch, heads, capacity, dim)
     for t in (cache.k, cache.v, cache.k_exps, cache.v_exps):
         t.fill_(255)
     if max(lengths) > 0:
         k, v = (_randn(gen, (batch, max(lengths), heads, dim)) for _ in range(2))
-        hb.cache_append(cache, k, v, _lens(lengths))
+        hb.cache_append(cache, k, values(v), _lens(lengths))
     k, v = hb.cache_read(cache, _lens(lengths))
     return cache, k.double(), v.double()
 
@@ -112,3 +112,34 @@ def test_bf16_outputs_lose_their_own_rounding_only(hb, batch, tokens, kv, group,
     q = _randn(gen, (batch, tokens, kv * group, dim), BF16)
     out, lse = hb.cache_attend(cache, q, _lens(lengths))
     _check_attend(out, lse, _attend64(k, v, q, lengths, dim ** -0.5), BF16, dim, capacity)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("batch,tokens,kv,group,dim,capacity,lengths", [
+    (2, 1, 2, 4, 64, 100, [100, 37]),
+    (1, 2, 1, 4, 128, 3000, [2999]),
+    (1, 60, 1, 2, 96, 1200, [1200]),
+    (2, 130, 1, 1, 64, 140, [140, 90]),
+])
+@pytest.mark.parametrize("power", [126, 60, -60])
+def test_values_of_every_magnitude(hb, dtype, batch, tokens, kv, group, dim, capacity, lengths, power):
+    """Values up to 2^127, all of one sign: sums of many weights times the largest stay finite, equal scores among them."""
+    print(f"[attend] values of 2^{power}: {dtype} b{batch} t{tokens} dim {dim} lengths {lengths}", flush=True)
+    gen = _gen(dim + tokens)
+    cache, k, v = _filled(hb, gen, batch, kv, capacity, dim, lengths, lambda x: (1 + x.abs().clamp(max=8) / 16) * 2.0 ** power)
+    q = _randn(gen, (batch, tokens, kv * group, dim), dtype)
+    q[:, :, 0] = 0
+    out, lse = hb.cache_attend(cache, q, _lens(lengths))
+    assert v.max() >= 2.0 ** power
+    _check_attend(out, lse, _attend64(k, v, q, lengths, dim ** -0.5), dtype, dim, capacity)
+
+
+def test_tiny_values_lose_an_absolute_amount_only(hb):
+    print("[attend] tiny values", flush=True)
+    gen = _gen(11)
+    for tokens in (1, 70):
+        cache, k, v = _filled(hb, gen, 1, 1, 300, 64, [300], lambda x: x * 2.0 ** -110)
+        q = _randn(gen, (1, tokens, 2, 64), F32)
+        out, _ = hb.cache_attend(cache, q, _lens([300]))
+        want = _attend64(k, v, q, [300], 0.125)
+        assert ((out.double() - want[0]).abs() <= 2.0 ** -90).all()
