@@ -679,12 +679,21 @@ def gemm_conv2d_dgrad(dy: BfpTensor, conv: Conv2d, filters: BfpTensor, out: Opti
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
-def _buffer(shape, dtype, device, stream) -> torch.Tensor:
-    """A tensor that a call on `stream` writes: the allocator must not hand its memory on before that stream is done with it."""
-    t = torch.empty(shape, dtype=dtype, device=device)
-    if stream is not None and t.numel():
-        t.record_stream(stream)
-    return t
+_current_device = getattr(torch._C, "_cuda_getDevice", None)      # (torch.cuda.current_device without its wrapper: half a microsecond)
+
+
+def _there(stream, device, call, *args):
+    """`call` on another stream, or on a device that is not the current one.  On a stream of its own a call's buffers come from that
+    stream's memory: a block that the caller's stream has freed may still be in use by work queued there, which the call does not
+    wait for; and the results are not handed on before the caller's stream is done with them."""
+    assert stream is None or stream.device == device, "a stream of the tensors' GPU"
+    caller = torch.cuda.current_stream(device)
+    with torch.cuda.device(device) if stream is None else torch.cuda.stream(stream):
+        result = call(*args)
+    for t in (result.codes, result.scales) if isinstance(result, RowCodes) else result if isinstance(result, tuple) else (result,):
+        if stream is not None and t is not None and t.numel():
+            t.record_stream(caller)
+    return result
 
 
 def _heads(t: torch.Tensor, batch: int, tokens: int, heads: int, dim: int, device) -> Heads:
@@ -700,10 +709,10 @@ def _lengths(lengths: torch.Tensor, batch: int, device) -> int:
     return lengths.data_ptr()
 
 
-def _raw_stream(stream, device) -> int:
-    """The stream a call goes to.  A decode step is a few microseconds of kernels, and a torch.cuda.Stream object for each of its calls
-    costs one of them; this is the handle alone."""
-    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+def _raw_stream(device) -> int:
+    """The current stream of a device.  A decode step is a few microseconds of kernels, and a torch.cuda.Stream object for each of its
+    calls costs one of them; this is the handle alone."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -750,21 +759,26 @@ def cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, lengths: torc
     """hbfp_cache_append: k, v [batch, tokens, heads, dim]; lengths (int32, on the GPU) count the new tokens.  values: returns the
     values that the cache now holds for them, a pair of bf16 tensors of k's shape."""
     d, tokens, device = cache.desc, k.shape[1], cache.k.device
+    if stream is not None or _current_device() != device.index:
+        return _there(stream, device, cache_append, cache, k, v, lengths, values)
     batch, heads, dim = d.batch, d.heads, d.dim
     hk, hv = _heads(k, batch, tokens, heads, dim, device), _heads(v, batch, tokens, heads, dim, device)
-    held = tuple(_buffer(k.shape, torch.bfloat16, device, stream) for _ in range(2)) if values else (None, None)
-    _check(_lib.hbfp_cache_append(ctypes.byref(d), ctypes.byref(hk), ctypes.byref(hv), tokens, _lengths(lengths, batch, device),
-                                  _ptr(held[0]), _ptr(held[1]), _raw_stream(stream, device)), "hbfp_cache_append")
+    at = _lengths(lengths, batch, device)
+    held = tuple(torch.empty(k.shape, dtype=torch.bfloat16, device=device) for _ in range(2)) if values else (None, None)
+    _check(_lib.hbfp_cache_append(ctypes.byref(d), ctypes.byref(hk), ctypes.byref(hv), tokens, at, _ptr(held[0]), _ptr(held[1]),
+                                  _raw_stream(device)), "hbfp_cache_append")
     return held if values else None
 
 
 def cache_read(cache: KvCache, lengths: torch.Tensor, dtype=torch.float32, stream=None):
     """hbfp_cache_read: (keys, values) [batch, heads, capacity, dim], 0 from each length on."""
     d, device = cache.desc, cache.k.device
+    if stream is not None or _current_device() != device.index:
+        return _there(stream, device, cache_read, cache, lengths, dtype)
     assert dtype in _TYPES
-    k, v = (_buffer((d.batch, d.heads, d.capacity, d.dim), dtype, device, stream) for _ in range(2))
-    _check(_lib.hbfp_cache_read(ctypes.byref(d), _lengths(lengths, d.batch, device), _TYPES[dtype], _ptr(k), _ptr(v),
-                                _raw_stream(stream, device)), "hbfp_cache_read")
+    at = _lengths(lengths, d.batch, device)
+    k, v = (torch.empty((d.batch, d.heads, d.capacity, d.dim), dtype=dtype, device=device) for _ in range(2))
+    _check(_lib.hbfp_cache_read(ctypes.byref(d), at, _TYPES[dtype], _ptr(k), _ptr(v), _raw_stream(device)), "hbfp_cache_read")
     return k, v
 
 
@@ -784,23 +798,23 @@ def cache_attend(cache: KvCache, q: torch.Tensor, lengths: torch.Tensor, scale: 
                  workspace: Optional[torch.Tensor] = None, stream=None):
     """hbfp_cache_attend: (out, lse) for q [batch, tokens, query heads, dim]; scale defaults to dim ** -0.5."""
     d, device = cache.desc, cache.k.device
+    if stream is not None or _current_device() != device.index:
+        return _there(stream, device, cache_attend, cache, q, lengths, scale, causal, longest, out, lse, workspace)
     batch, dim = d.batch, d.dim
     _, tokens, heads, _ = q.shape
-    hq = _heads(q, batch, tokens, heads, dim, device)
+    hq, at = _heads(q, batch, tokens, heads, dim, device), _lengths(lengths, batch, device)
     if out is None:
-        out = _buffer(q.shape, q.dtype, device, stream)
+        out = torch.empty(q.shape, dtype=q.dtype, device=device)
     if lse is None:
-        lse = _buffer((batch, tokens, heads), torch.float32, device, stream)
+        lse = torch.empty((batch, tokens, heads), dtype=torch.float32, device=device)
     else:
         assert lse.device == device and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (batch, tokens, heads)
     ho = _heads(out, batch, tokens, heads, dim, device)
     if workspace is None:
-        need = _attend_bytes(batch, d.heads, d.capacity, dim, tokens, heads, hq.dtype, longest)
-        workspace = _buffer((need,), torch.uint8, device, stream) if need else None
-    _check(_lib.hbfp_cache_attend(ctypes.byref(d), ctypes.byref(hq), tokens, heads, _lengths(lengths, batch, device), longest,
-                                  dim ** -0.5 if scale is None else scale, 1 if causal else 0, ctypes.byref(ho), _ptr(lse),
-                                  _ptr(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(stream, device)),
-           "hbfp_cache_attend")
+        workspace = _workspace(_attend_bytes(batch, d.heads, d.capacity, dim, tokens, heads, hq.dtype, longest), device)
+    _check(_lib.hbfp_cache_attend(ctypes.byref(d), ctypes.byref(hq), tokens, heads, at, longest, dim ** -0.5 if scale is None else scale,
+                                  1 if causal else 0, ctypes.byref(ho), _ptr(lse), _ptr(workspace),
+                                  0 if workspace is None else workspace.numel(), _raw_stream(device)), "hbfp_cache_attend")
     return out, lse
 
 
@@ -810,6 +824,8 @@ def cache_weigh(cache: KvCache, q: torch.Tensor, lse: torch.Tensor, lengths: tor
     """hbfp_cache_weigh: out = decay * weights + the attention weight each cached token received; weights FP32 [batch, heads, n],
     n >= capacity; out defaults to weights (in place)."""
     d, device = cache.desc, cache.k.device
+    if stream is not None or _current_device() != device.index:
+        return _there(stream, device, cache_weigh, cache, q, lse, lengths, weights, scale, causal, decay, out)
     batch, dim = d.batch, d.dim
     _, tokens, heads, _ = q.shape
     hq = _heads(q, batch, tokens, heads, dim, device)
@@ -818,9 +834,10 @@ def cache_weigh(cache: KvCache, q: torch.Tensor, lse: torch.Tensor, lengths: tor
         assert t.device == device and t.dtype == torch.float32 and t.is_contiguous() and t.shape == weights.shape
     assert weights.dim() == 3 and weights.shape[0] == batch and weights.shape[1] == d.heads
     assert lse.device == device and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (batch, tokens, heads)
-    _check(_lib.hbfp_cache_weigh(ctypes.byref(d), ctypes.byref(hq), tokens, heads, _lengths(lengths, batch, device),
-                                 dim ** -0.5 if scale is None else scale, 1 if causal else 0, _ptr(lse), decay, _ptr(weights),
-                                 _ptr(out), weights.shape[2], _raw_stream(stream, device)), "hbfp_cache_weigh")
+    at = _lengths(lengths, batch, device)
+    _check(_lib.hbfp_cache_weigh(ctypes.byref(d), ctypes.byref(hq), tokens, heads, at, dim ** -0.5 if scale is None else scale,
+                                 1 if causal else 0, _ptr(lse), decay, _ptr(weights), _ptr(out), weights.shape[2],
+                                 _raw_stream(device)), "hbfp_cache_weigh")
     return out
 
 
@@ -828,17 +845,20 @@ def cache_evict(cache: KvCache, weights: torch.Tensor, lengths: torch.Tensor, ou
                 out_weights: Optional[torch.Tensor] = None, stream=None):
     """hbfp_cache_evict into the cache `out`: (kept slots [batch, heads, keep], new lengths, their weights [batch, heads, n])."""
     d, device = cache.desc, cache.k.device
+    if stream is not None or _current_device() != device.index:
+        return _there(stream, device, cache_evict, cache, weights, lengths, out, keep, recent, out_weights)
     assert weights.device == device and weights.dtype == torch.float32 and weights.is_contiguous() and weights.dim() == 3
     assert weights.shape[:2] == (d.batch, d.heads) and out.k.device == device
+    at = _lengths(lengths, d.batch, device)
     if out_weights is None:
-        out_weights = _buffer((d.batch, d.heads, out.desc.capacity), torch.float32, device, stream)
+        out_weights = torch.empty((d.batch, d.heads, out.desc.capacity), dtype=torch.float32, device=device)
     assert out_weights.device == device and out_weights.dtype == torch.float32 and out_weights.is_contiguous() and out_weights.dim() == 3
     assert out_weights.shape[:2] == (d.batch, d.heads)
-    kept = _buffer((d.batch, d.heads, max(keep, 1)), torch.int32, device, stream)
-    new_lengths = _buffer((d.batch,), torch.int32, device, stream)
-    _check(_lib.hbfp_cache_evict(ctypes.byref(d), _ptr(weights), weights.shape[2], _lengths(lengths, d.batch, device), keep, recent,
-                                 ctypes.byref(out.desc), _ptr(out_weights), out_weights.shape[2], _ptr(kept),
-                                 _ptr(new_lengths), _raw_stream(stream, device)), "hbfp_cache_evict")
+    kept = torch.empty((d.batch, d.heads, max(keep, 1)), dtype=torch.int32, device=device)
+    new_lengths = torch.empty((d.batch,), dtype=torch.int32, device=device)
+    _check(_lib.hbfp_cache_evict(ctypes.byref(d), _ptr(weights), weights.shape[2], at, keep, recent, ctypes.byref(out.desc),
+                                 _ptr(out_weights), out_weights.shape[2], _ptr(kept), _ptr(new_lengths), _raw_stream(device)),
+           "hbfp_cache_evict")
     return kept, new_lengths, out_weights
 
 
@@ -859,22 +879,24 @@ def _matrix(t: torch.Tensor):
 def quant_rows(x: torch.Tensor, stream=None) -> RowCodes:
     """hbfp_quant_rows of x [rows, cols]: a linear layer's weights [out features, in features], once; or tokens."""
     ld = _matrix(x)
+    if stream is not None or _current_device() != x.device.index:
+        return _there(stream, x.device, quant_rows, x)
     kpad = ctypes.c_int64(0)
     _check(_lib.hbfp_rows_plan(x.shape[0], x.shape[1], ctypes.byref(kpad), None), "hbfp_rows_plan")
-    codes = _buffer((x.shape[0], kpad.value), torch.int8, x.device, stream)
-    scales = _buffer((x.shape[0],), torch.float32, x.device, stream)
+    codes = torch.empty((x.shape[0], kpad.value), dtype=torch.int8, device=x.device)
+    scales = torch.empty((x.shape[0],), dtype=torch.float32, device=x.device)
     _check(_lib.hbfp_quant_rows(_ptr(x), _TYPES[x.dtype], x.shape[0], x.shape[1], ld, _ptr(codes), _ptr(scales),
-                                _raw_stream(stream, x.device)), "hbfp_quant_rows")
+                                _raw_stream(x.device)), "hbfp_quant_rows")
     return RowCodes(codes, scales, x.shape[1])
 
 
-def _product_out(bias, w: RowCodes, rows: int, dtype, device, out, stream):
+def _product_out(bias, w: RowCodes, rows: int, dtype, device, out):
     n = w.codes.shape[0]
     assert w.codes.device == device
     if bias is not None:
         assert bias.device == device and bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == n
     if out is None:
-        out = _buffer((rows, n), dtype, device, stream)
+        out = torch.empty((rows, n), dtype=dtype, device=device)
     assert out.device == device and out.dtype == dtype and tuple(out.shape) == (rows, n)
     return out, _matrix(out)
 
@@ -898,13 +920,14 @@ def gemm_rows(a: RowCodes, w: RowCodes, bias: Optional[torch.Tensor] = None, dty
     """hbfp_gemm_rows: y [rows of a, rows of w] = a . w^T (+ bias), rounded once to `dtype`."""
     assert a.cols == w.cols
     m, n, device = a.codes.shape[0], w.codes.shape[0], a.codes.device
-    out, ld = _product_out(bias, w, m, dtype if out is None else out.dtype, device, out, stream)
+    if stream is not None or _current_device() != device.index:
+        return _there(stream, device, gemm_rows, a, w, bias, dtype, out, workspace)
+    out, ld = _product_out(bias, w, m, dtype if out is None else out.dtype, device, out)
     if workspace is None:
-        need = gemm_rows_workspace(m, n, a.cols)
-        workspace = _buffer((need,), torch.uint8, device, stream) if need else None
+        workspace = _workspace(gemm_rows_workspace(m, n, a.cols), device)
     _check(_lib.hbfp_gemm_rows(_ptr(a.codes), _ptr(a.scales), _ptr(w.codes), _ptr(w.scales), _ptr(bias), m, n, a.cols,
                                _ptr(out), _TYPES[out.dtype], ld, _ptr(workspace), 0 if workspace is None else workspace.numel(),
-                               _raw_stream(stream, device)), "hbfp_gemm_rows")
+                               _raw_stream(device)), "hbfp_gemm_rows")
     return out
 
 
@@ -912,11 +935,13 @@ def linear_i8(x: torch.Tensor, w: RowCodes, bias: Optional[torch.Tensor] = None,
               workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """hbfp_linear_i8: y = quant(x) . w^T (+ bias) in x's type, for x [tokens, in features] and weights from quant_rows."""
     ldx, (m, k), n = _matrix(x), x.shape, w.codes.shape[0]
+    if stream is not None or _current_device() != x.device.index:
+        return _there(stream, x.device, linear_i8, x, w, bias, out, workspace)
     assert k == w.cols
-    out, ldy = _product_out(bias, w, m, x.dtype, x.device, out, stream)
+    out, ldy = _product_out(bias, w, m, x.dtype, x.device, out)
     if workspace is None:
-        need = linear_i8_workspace(m, n, k)
-        workspace = _buffer((need,), torch.uint8, x.device, stream) if need else None
-    _check(_lib.hbfp_linear_i8(_ptr(x), _TYPES[x.dtype], m, k, ldx, _ptr(w.codes), _ptr(w.scales), _ptr(bias), n,
-                               _ptr(out), ldy, _ptr(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(stream, x.device)), "hbfp_linear_i8")
+        workspace = _workspace(linear_i8_workspace(m, n, k), x.device)
+    _check(_lib.hbfp_linear_i8(_ptr(x), _TYPES[x.dtype], m, k, ldx, _ptr(w.codes), _ptr(w.scales), _ptr(bias), n, _ptr(out), ldy,
+                               _ptr(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(x.device)),
+           "hbfp_linear_i8")
     return out

@@ -143,3 +143,30 @@ def test_tiny_values_lose_an_absolute_amount_only(hb):
         out, _ = hb.cache_attend(cache, q, _lens([300]))
         want = _attend64(k, v, q, [300], 0.125)
         assert ((out.double() - want[0]).abs() <= 2.0 ** -90).all()
+
+
+# --------------------------------------------------------------------------------------------------------------- streams
+def test_results_on_another_stream_do_not_take_memory_in_use(hb):
+    """The caller's stream still has a kernel queued that reads a tensor just dropped; a call on another stream does not wait for it."""
+    print("[streams] memory in use", flush=True)
+    gen = _gen(12)
+    x, w = _randn(gen, (512, 256), BF16), hb.quant_rows(_randn(gen, (2048, 256)))
+    negative = -x                                              # (inputs are ready before the other stream is used)
+    want = hb.linear_i8(x, w)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    dropped = torch.full((512, 2048), 3.0, device="cuda", dtype=BF16)
+    torch.cuda._sleep(100_000_000)                             # tens of milliseconds
+    twice = dropped * 2
+    del dropped
+    got = hb.linear_i8(x, w, stream=side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert (twice == 6).all() and torch.equal(got, want)
+    # a result that the caller's stream still reads when it is dropped is not given to the other stream's next call
+    torch.cuda._sleep(100_000_000)
+    twice = got * 2
+    del got
+    again = hb.linear_i8(negative, w, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(twice, want * 2) and torch.equal(again, -want)
