@@ -773,9 +773,14 @@ int hbfp_cache_attend(const hbfp_cache *cache, const hbfp_heads *q, int64_t toke
  *   w_out[b][h][j] = decay * w_in[b][h][j] + sum over the call's tokens and the query heads of key head h of exp(s[j] - lse)
  * for j < lengths[b], 0 for j from there to the capacity.  q, tokens, heads, lengths, scale, causal and lse as in (and from)
  * hbfp_cache_attend; w_in and w_out are FP32 [batch][cache->heads][ld], ld >= capacity; w_out may be w_in.
+ * lse has to come from queries that saw every key here: hbfp_cache_attend with `longest` 0 or at least every length.  For any other,
+ * hbfp_cache_weigh_longest takes the same `longest`: keys from it on are not seen, and receive decay * w_in alone.
  */
 int hbfp_cache_weigh(const hbfp_cache *cache, const hbfp_heads *q, int64_t tokens, int64_t heads, const int32_t *lengths, float scale,
                      int causal, const float *lse, float decay, const float *w_in, float *w_out, int64_t ld, void *stream);
+int hbfp_cache_weigh_longest(const hbfp_cache *cache, const hbfp_heads *q, int64_t tokens, int64_t heads, const int32_t *lengths,
+                             int64_t longest, float scale, int causal, const float *lse, float decay, const float *w_in, float *w_out,
+                             int64_t ld, void *stream);
 
 /*
  * hbfp_cache_evict: copies of every head the tokens that matter into another cache (one spare cache serves all layers of a

@@ -394,7 +394,7 @@ __global__ __launch_bounds__(256) void cache_weigh_kernel(const WeighParams p) {
         const int row = 16 * tile + c;
         limit = 0;
         if (row < p.rows) {
-            limit = visible(length, p.a.tokens, p.a.group, row, p.a.causal, bound);
+            limit = visible(length, p.a.tokens, p.a.group, row, p.a.causal, p.a.longest);
             lse2 = p.a.lse[(b * p.a.tokens + row / p.a.group) * p.a.heads + key_head * p.a.group + row % p.a.group] * kLog2e;
         }
         load_queries<NB, DT>(p.a.q, b, key_head, p.a.group, row, p.rows, cache.dim, g, false, q);
@@ -427,7 +427,7 @@ __global__ __launch_bounds__(256) void cache_weigh_kernel(const WeighParams p) {
         for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
         for (int tile = 0; tile < p.tiles; ++tile) {
             const int last_row = 16 * tile + 15 < p.rows ? 16 * tile + 15 : p.rows - 1;
-            if (visible(length, p.a.tokens, p.a.group, last_row, p.a.causal, bound) <= key0) continue;
+            if (visible(length, p.a.tokens, p.a.group, last_row, p.a.causal, p.a.longest) <= key0) continue;
             if (p.tiles > 1) load_tile(tile);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {

@@ -56,7 +56,7 @@ struct WeighArgs {
     const float *lse, *w_in;
     float *w_out;
     int64_t ld;
-    int32_t tokens, heads, group, causal;
+    int32_t tokens, heads, group, causal, longest;
     float scale, decay;
 };
 int launch_cache_weigh(const WeighArgs &a, int dtype, hipStream_t s);

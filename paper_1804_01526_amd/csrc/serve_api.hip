@@ -76,6 +76,8 @@ int check_queries(const hbfp_cache *c, int64_t tokens, int64_t heads) {
     return HBFP_OK;
 }
 
+int32_t longest_of(const hbfp_cache *c, int64_t longest) { return (int32_t)(longest == 0 || longest > c->capacity ? c->capacity : longest); }
+
 int attend_args(const hbfp_cache *cache, int64_t tokens, int64_t heads, int64_t longest, AttendArgs *a) {
     const int rc = check_queries(cache, tokens, heads);
     if (rc != HBFP_OK) return rc;
@@ -85,7 +87,7 @@ int attend_args(const hbfp_cache *cache, int64_t tokens, int64_t heads, int64_t 
     a->tokens = (int32_t)tokens;
     a->heads = (int32_t)heads;
     a->group = (int32_t)(heads / cache->heads);
-    a->longest = (int32_t)(longest == 0 || longest > cache->capacity ? cache->capacity : longest);
+    a->longest = longest_of(cache, longest);
     return HBFP_OK;
 }
 
@@ -166,11 +168,13 @@ int hbfp_cache_attend(const hbfp_cache *cache, const hbfp_heads *q, int64_t toke
     return launch_cache_attend(a, q->dtype, (hipStream_t)stream);
 }
 
-int hbfp_cache_weigh(const hbfp_cache *cache, const hbfp_heads *q, int64_t tokens, int64_t heads, const int32_t *lengths, float scale,
-                     int causal, const float *lse, float decay, const float *w_in, float *w_out, int64_t ld, void *stream) {
+int hbfp_cache_weigh_longest(const hbfp_cache *cache, const hbfp_heads *q, int64_t tokens, int64_t heads, const int32_t *lengths,
+                             int64_t longest, float scale, int causal, const float *lse, float decay, const float *w_in, float *w_out,
+                             int64_t ld, void *stream) {
     int rc = check_cache(cache);
     if (rc != HBFP_OK) return rc;
     if ((rc = check_queries(cache, tokens, heads)) != HBFP_OK) return rc;
+    if (longest < 0) return HBFP_ERR_ARG;
     if ((rc = check_heads(q, cache->batch, tokens, heads, cache->dim, false)) != HBFP_OK) return rc;
     if (!lengths || !lse || !w_in || !w_out || ld < cache->capacity || (causal != 0 && causal != 1)) return HBFP_ERR_ARG;
     if (((uintptr_t)lengths | (uintptr_t)lse | (uintptr_t)w_in | (uintptr_t)w_out) & 3) return HBFP_ERR_ARG;
@@ -178,8 +182,13 @@ int hbfp_cache_weigh(const hbfp_cache *cache, const hbfp_heads *q, int64_t token
     const uint64_t span = 4 * ((uint64_t)(cache->batch * cache->heads - 1) * (uint64_t)ld + (uint64_t)cache->capacity);
     if (w_in != w_out && overlap(w_in, span, w_out, span)) return HBFP_ERR_ARG;
     WeighArgs a = {view_of(*cache), heads_of(*q), lengths, lse, w_in, w_out, ld, (int32_t)tokens, (int32_t)heads, (int32_t)(heads / cache->heads),
-                   causal, scale, decay};
+                   causal, longest_of(cache, longest), scale, decay};
     return launch_cache_weigh(a, q->dtype, (hipStream_t)stream);
+}
+
+int hbfp_cache_weigh(const hbfp_cache *cache, const hbfp_heads *q, int64_t tokens, int64_t heads, const int32_t *lengths, float scale,
+                     int causal, const float *lse, float decay, const float *w_in, float *w_out, int64_t ld, void *stream) {
+    return hbfp_cache_weigh_longest(cache, q, tokens, heads, lengths, 0, scale, causal, lse, decay, w_in, w_out, ld, stream);
 }
 
 int hbfp_cache_evict(const hbfp_cache *src, const float *w, int64_t ld, const int32_t *lengths, int64_t keep, int64_t recent,

@@ -149,6 +149,7 @@ def _load():
     lib.hbfp_cache_attend_workspace.argtypes = [KV, i64, i64, i32, i64, ctypes.POINTER(sz)]
     lib.hbfp_cache_attend.argtypes = [KV, H, i64, i64, vp, i64, f32, i32, H, vp, vp, sz, vp]
     lib.hbfp_cache_weigh.argtypes = [KV, H, i64, i64, vp, f32, i32, vp, f32, vp, vp, i64, vp]
+    lib.hbfp_cache_weigh_longest.argtypes = [KV, H, i64, i64, vp, i64, f32, i32, vp, f32, vp, vp, i64, vp]
     lib.hbfp_cache_evict.argtypes = [KV, vp, i64, vp, i64, i64, KV, vp, i64, vp, vp, vp]
     lib.hbfp_rows_plan.argtypes = [i64, i64, ctypes.POINTER(i64), ctypes.POINTER(sz)]
     lib.hbfp_quant_rows.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
@@ -157,7 +158,7 @@ def _load():
     lib.hbfp_linear_i8_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(sz)]
     lib.hbfp_linear_i8.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, i64, vp, i64, vp, sz, vp]
     for name in ("hbfp_cache_plan", "hbfp_cache_append", "hbfp_cache_read", "hbfp_cache_attend_workspace", "hbfp_cache_attend",
-                 "hbfp_cache_weigh", "hbfp_cache_evict", "hbfp_rows_plan", "hbfp_quant_rows", "hbfp_gemm_rows_workspace",
+                 "hbfp_cache_weigh", "hbfp_cache_weigh_longest", "hbfp_cache_evict", "hbfp_rows_plan", "hbfp_quant_rows", "hbfp_gemm_rows_workspace",
                  "hbfp_gemm_rows", "hbfp_linear_i8_workspace", "hbfp_linear_i8"):
         getattr(lib, name).restype = i32
     for name in ("hbfp_gemm_batch_workspace", "hbfp_gemm_batch", "hbfp_gemm_bfp_workspace", "hbfp_gemm_bfp", "hbfp_encode_im2col", "hbfp_encode_multi_workspace", "hbfp_encode_multi", "hbfp_encode_packed_workspace", "hbfp_encode_packed", "hbfp_encode_packed_batch_workspace", "hbfp_encode_packed_batch", "hbfp_weight_update_workspace", "hbfp_weight_update", "hbfp_plan", "hbfp_encode_workspace", "hbfp_encode", "hbfp_encode_static", "hbfp_decode", "hbfp_gemm_workspace",
@@ -820,12 +821,12 @@ def cache_attend(cache: KvCache, q: torch.Tensor, lengths: torch.Tensor, scale: 
 
 def cache_weigh(cache: KvCache, q: torch.Tensor, lse: torch.Tensor, lengths: torch.Tensor, weights: torch.Tensor,
                 scale: Optional[float] = None, causal: bool = True, decay: float = 1.0, out: Optional[torch.Tensor] = None,
-                stream=None) -> torch.Tensor:
+                stream=None, longest: int = 0) -> torch.Tensor:
     """hbfp_cache_weigh: out = decay * weights + the attention weight each cached token received; weights FP32 [batch, heads, n],
-    n >= capacity; out defaults to weights (in place)."""
+    n >= capacity; out defaults to weights (in place).  longest: that of the attention call that lse comes from."""
     d, device = cache.desc, cache.k.device
     if stream is not None or _current_device() != device.index:
-        return _there(stream, device, cache_weigh, cache, q, lse, lengths, weights, scale, causal, decay, out)
+        return _there(stream, device, cache_weigh, cache, q, lse, lengths, weights, scale, causal, decay, out, None, longest)
     batch, dim = d.batch, d.dim
     _, tokens, heads, _ = q.shape
     hq = _heads(q, batch, tokens, heads, dim, device)
@@ -835,9 +836,9 @@ def cache_weigh(cache: KvCache, q: torch.Tensor, lse: torch.Tensor, lengths: tor
     assert weights.dim() == 3 and weights.shape[0] == batch and weights.shape[1] == d.heads
     assert lse.device == device and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (batch, tokens, heads)
     at = _lengths(lengths, batch, device)
-    _check(_lib.hbfp_cache_weigh(ctypes.byref(d), ctypes.byref(hq), tokens, heads, at, dim ** -0.5 if scale is None else scale,
-                                 1 if causal else 0, _ptr(lse), decay, _ptr(weights), _ptr(out), weights.shape[2],
-                                 _raw_stream(device)), "hbfp_cache_weigh")
+    _check(_lib.hbfp_cache_weigh_longest(ctypes.byref(d), ctypes.byref(hq), tokens, heads, at, longest, dim ** -0.5 if scale is None else scale,
+                                         1 if causal else 0, _ptr(lse), decay, _ptr(weights), _ptr(out), weights.shape[2],
+                                         _raw_stream(device)), "hbfp_cache_weigh_longest")
     return out
 
 

@@ -170,3 +170,30 @@ def test_results_on_another_stream_do_not_take_memory_in_use(hb):
     again = hb.linear_i8(negative, w, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(twice, want * 2) and torch.equal(again, -want)
+
+
+# --------------------------------------------------------------------------------------------------------------- weights
+@pytest.mark.parametrize("dtype,tokens,dim,lengths,longest,causal", [
+    (F32, 1, 64, [900, 20], 100, True),
+    (BF16, 5, 128, [300, 299], 256, False),
+    (F16, 40, 40, [700, 333], 640, True),
+    (F32, 2, 32, [500, 120], 130, False),
+    (BF16, 3, 96, [260, 1], 10 ** 9, True),
+])
+def test_weights_of_a_call_that_sees_the_first_keys_only(hb, dtype, tokens, dim, lengths, longest, causal):
+    """cache_weigh with the `longest` of the attention call before it: a query's weights sum to 1, keys from there on receive none."""
+    print(f"[weigh] longest {longest} of {lengths}, {dtype} t{tokens} dim {dim}", flush=True)
+    gen, kv, group, capacity = _gen(13), 2, 3, 1000
+    cache, k, v = _filled(hb, gen, 2, kv, capacity, dim, lengths)
+    q = _randn(gen, (2, tokens, kv * group, dim), dtype)
+    _, lse = hb.cache_attend(cache, q, _lens(lengths), causal=causal, longest=longest)
+    before = torch.rand((2, kv, capacity), generator=gen, device="cuda")
+    w = hb.cache_weigh(cache, q, lse, _lens(lengths), before, causal=causal, decay=0.5, out=torch.full_like(before, 9.0), longest=longest)
+    _, want_lse, _, noise, got = _attend64(k, v, q, lengths, dim ** -0.5, causal, longest)
+    for b, n in enumerate(lengths):
+        want = 0.5 * before[b].double() + got[b]
+        want[:, n:] = 0
+        seen = want_lse[b][torch.isfinite(want_lse[b])]
+        d = (dim + 16) * 2.0 ** -24 * noise[b].max() + (64 + capacity / 32) * 2.0 ** -24 + 2.0 ** -21 * (1 + seen.abs().max())
+        assert ((w[b].double() - want).abs() <= (2 * d + tokens * group * 2.0 ** -24) * want).all()
+        assert torch.equal(w[b, :, min(longest, n):n], 0.5 * before[b, :, min(longest, n):n])

@@ -23,7 +23,7 @@ def _calls(hb):
         "hbfp_cache_append": lambda s: hb.cache_append(cache, new, new, lengths, values=True, stream=s),
         "hbfp_cache_read": lambda s: hb.cache_read(cache, lengths, stream=s),
         "hbfp_cache_attend": lambda s: hb.cache_attend(cache, q, lengths, stream=s),
-        "hbfp_cache_weigh": lambda s: hb.cache_weigh(cache, q, lse, lengths, weights, stream=s),
+        "hbfp_cache_weigh_longest": lambda s: hb.cache_weigh(cache, q, lse, lengths, weights, stream=s),
         "hbfp_cache_evict": lambda s: hb.cache_evict(cache, weights, lengths, spare, 10, 5, stream=s),
         "hbfp_quant_rows": lambda s: hb.quant_rows(x, stream=s),
         "hbfp_gemm_rows": lambda s: hb.gemm_rows(rows, codes, stream=s),
@@ -31,7 +31,7 @@ def _calls(hb):
     }
 
 
-NAMES = ["hbfp_cache_append", "hbfp_cache_read", "hbfp_cache_attend", "hbfp_cache_weigh", "hbfp_cache_evict", "hbfp_quant_rows", "hbfp_gemm_rows",
+NAMES = ["hbfp_cache_append", "hbfp_cache_read", "hbfp_cache_attend", "hbfp_cache_weigh_longest", "hbfp_cache_evict", "hbfp_quant_rows", "hbfp_gemm_rows",
          "hbfp_linear_i8"]
 
 
@@ -72,7 +72,7 @@ def test_a_call_on_a_stream_allocates_there(recorded, name):
     calls[name](side)
     assert [e for e in log if e[0] == "launch"] == [("launch", side, side)]
     assert all(e[1] is side for e in log if e[0] == "alloc")
-    outputs = {"hbfp_cache_weigh": 1, "hbfp_cache_evict": 3, "hbfp_gemm_rows": 1, "hbfp_linear_i8": 1}.get(name, 2)
+    outputs = {"hbfp_cache_weigh_longest": 1, "hbfp_cache_evict": 3, "hbfp_gemm_rows": 1, "hbfp_linear_i8": 1}.get(name, 2)
     assert [e for e in log if e[0] == "record"] == [("record", "the caller's stream")] * outputs
 
 
@@ -92,3 +92,14 @@ def test_a_stream_of_another_device_is_refused(recorded):
     side.device = torch.device("meta")
     with pytest.raises(AssertionError):
         recorded[0]["hbfp_quant_rows"](side)
+
+
+def test_weigh_longest_refusals():
+    import ctypes
+    at = 0x100000                                              # nothing reads it: every call below is refused on the host
+    c = hbfp.cache_plan(2, 2, 100, 64)
+    c.k, c.v, c.k_exps, c.v_exps = at, at + (1 << 24), at + (2 << 24), at + (3 << 24)
+    q = hbfp.Heads(at, 1, 0, 1024, 256, 64)
+    weigh = lambda longest=0, ld=100, w=at, heads=8: hbfp._lib.hbfp_cache_weigh_longest(
+        ctypes.byref(c), ctypes.byref(q), 1, heads, at, longest, 0.1, 1, at, 1.0, w, at, ld, None)
+    assert weigh(longest=-1) == hbfp.ERR_ARG and weigh(ld=99) == hbfp.ERR_ARG and weigh(w=None) == hbfp.ERR_ARG and weigh(heads=7) == hbfp.ERR_ARG
