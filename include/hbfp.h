@@ -710,6 +710,8 @@ int hbfp_probe_matrix_rate(int instruction, const int *words, int workgroups, in
  *
  * Tensors of one call's tokens, [batch][tokens][heads][dim], are given as hbfp_heads: dim is contiguous, the other strides are
  * free (slices of one projection; an input may be broadcast with stride 0).  Types: HBFP_F32, HBFP_BF16, HBFP_F16.
+ * An output's elements may not be an input's or another output's, except as stated below and that attention may write `out` over q,
+ * element by element (same pointer, same strides).
  */
 enum { HBFP_F32 = 0, HBFP_BF16 = 1, HBFP_F16 = 2 };
 
@@ -813,7 +815,8 @@ int hbfp_quant_rows(const void *src, int dtype, int64_t rows, int64_t cols, int6
  * hbfp_gemm_rows: Y[m][n] = (sum_k a[m][k] b[n][k]) * a_scales[m] * b_scales[n] + bias[n], the sum an exact int32, the rest FP32
  * with Y rounded once to its type.  a: M rows (tokens), b: N rows (channels), both of K codes in rows of kpad bytes, 16-byte
  * aligned.  bias: FP32 [N] or NULL.  y: [M][ldy], ldy >= N.
- * hbfp_linear_i8: hbfp_quant_rows of x and the product in one call; Y has x's type.
+ * hbfp_linear_i8: hbfp_quant_rows of x and the product in one call; Y has x's type.  Rows of y may not overlap rows of x (refused with
+ * HBFP_ERR_ARG where the call reads x and writes y in one launch); both may be columns of one matrix.
  * workspace: the matching _workspace bytes, 256-byte aligned.
  * Errors: HBFP_ERR_ARG, HBFP_ERR_FORMAT (dtype), HBFP_ERR_RANGE (K * 127^2 reaches 2^31: K > 133144), HBFP_ERR_WORKSPACE,
  * HBFP_ERR_LAUNCH.

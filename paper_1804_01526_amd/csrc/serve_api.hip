@@ -278,6 +278,11 @@ int hbfp_linear_i8(const void *x, int dtype, int64_t M, int64_t K, int64_t ldx, 
     if (!b || !b_scales || ((uintptr_t)b & 15) || (((uintptr_t)b_scales | (uintptr_t)bias) & 3)) return HBFP_ERR_ARG;
     const int64_t kpad = round_up(K, 128);
     if (linear_fused_ok(M, N, kpad)) {
+        // every workgroup reads all of x for itself, while others store their part of y
+        const int64_t size = dtype == HBFP_F32 ? 4 : 2;
+        for (int64_t i = 0; i < M; ++i)
+            for (int64_t j = 0; j < M; ++j)
+                if (overlap((const uint8_t *)y + i * ldy * size, N * size, (const uint8_t *)x + j * ldx * size, K * size)) return HBFP_ERR_ARG;
         const RowsArgs r = {nullptr, b, nullptr, b_scales, bias, y, M, N, K, kpad, ldy, dtype};
         return launch_linear_fused(r, x, ldx, (hipStream_t)stream);
     }

@@ -197,3 +197,21 @@ def test_weights_of_a_call_that_sees_the_first_keys_only(hb, dtype, tokens, dim,
         d = (dim + 16) * 2.0 ** -24 * noise[b].max() + (64 + capacity / 32) * 2.0 ** -24 + 2.0 ** -21 * (1 + seen.abs().max())
         assert ((w[b].double() - want).abs() <= (2 * d + tokens * group * 2.0 ** -24) * want).all()
         assert torch.equal(w[b, :, min(longest, n):n], 0.5 * before[b, :, min(longest, n):n])
+
+
+# -------------------------------------------------------------------------------------------------------------- products
+def test_linear_between_columns_of_one_matrix_and_attention_over_its_queries(hb):
+    """Inputs and outputs that interleave in memory without sharing an element; out written over q."""
+    print("[linear] columns of one matrix", flush=True)
+    gen = _gen(14)
+    w = hb.quant_rows(_randn(gen, (200, 300)))
+    for m in (1, 2, 5, 40):
+        both = _randn(gen, (m, 504), BF16)
+        x, y = both[:, :300], both[:, 304:]
+        want, kept = hb.linear_i8(x.clone(), w), x.clone()
+        assert torch.equal(hb.linear_i8(x, w, out=y), want) and torch.equal(x, kept)
+    for tokens, capacity in ((1, 90), (1, 5000), (80, 90), (70, 2000)):
+        cache, _, _ = _filled(hb, gen, 1, 2, capacity, 64, [capacity])
+        q = _randn(gen, (1, tokens, 8, 64), BF16)
+        want = hb.cache_attend(cache, q, _lens([capacity]))[0]
+        assert torch.equal(hb.cache_attend(cache, q, _lens([capacity]), out=q)[0], want)

@@ -103,3 +103,12 @@ def test_weigh_longest_refusals():
     weigh = lambda longest=0, ld=100, w=at, heads=8: hbfp._lib.hbfp_cache_weigh_longest(
         ctypes.byref(c), ctypes.byref(q), 1, heads, at, longest, 0.1, 1, at, 1.0, w, at, ld, None)
     assert weigh(longest=-1) == hbfp.ERR_ARG and weigh(ld=99) == hbfp.ERR_ARG and weigh(w=None) == hbfp.ERR_ARG and weigh(heads=7) == hbfp.ERR_ARG
+
+
+def test_linear_refuses_to_write_the_tokens_it_still_reads():
+    at = 0x100000
+    lin = lambda x, y, m, k, n, ldx, ldy, dtype=1: hbfp._lib.hbfp_linear_i8(x, dtype, m, k, ldx, at + (1 << 28), at + (2 << 28), None, n, y, ldy, None, 0, None)
+    for m, k, n, ldx, ldy, shift in ((1, 256, 256, 256, 256, 0), (1, 256, 64, 256, 64, 510), (1, 64, 256, 64, 256, -510),
+                                     (2, 512, 100, 512, 512, 1024), (2, 512, 100, 700, 300, 1400), (2, 300, 300, 300, 600, 2 * 599)):
+        assert hbfp.linear_i8_workspace(m, n, k) == 0
+        assert lin(at, at + shift, m, k, n, ldx, ldy) == hbfp.ERR_ARG, (m, k, n, shift)
