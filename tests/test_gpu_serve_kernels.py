@@ -11,6 +11,8 @@ import numpy as np
 import pytest
 import torch
 
+from tests.util import launched_kernels
+
 pytestmark = pytest.mark.gpu
 
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
@@ -215,3 +217,142 @@ def test_linear_between_columns_of_one_matrix_and_attention_over_its_queries(hb)
         q = _randn(gen, (1, tokens, 8, 64), BF16)
         want = hb.cache_attend(cache, q, _lens([capacity]))[0]
         assert torch.equal(hb.cache_attend(cache, q, _lens([capacity]), out=q)[0], want)
+
+
+PROMPTS = [
+    # rows a workgroup, batch, tokens, key heads, group, capacity, lengths, causal
+    (256, 4, 129, 16, 4, 1100, [1100, 600, 129, 50], True),          # three chunks; a last tile of 4 rows; padding on the left
+    (256, 8, 300, 16, 2, 500, [500, 499, 300, 299, 1, 0, 64, 333], True),    # one chunk; conversations of no token, of one
+    (256, 4, 200, 16, 2, 1300, [1290, 65, 0, 1024], False),
+    (128, 4, 100, 16, 1, 2100, [2100, 1111, 100, 3], True),
+    (128, 16, 60, 16, 2, 400, [400 - 26 * i for i in range(16)], True),      # one chunk
+    (128, 16, 35, 16, 3, 260, [0, 1, 257] + [20 * i for i in range(13)], False),
+    (64, 1, 50, 2, 3, 300, [277], True),
+    (64, 2, 66, 1, 1, 1700, [1700, 30], True),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("dim", [32, 41, 96, 128])
+@pytest.mark.parametrize("rows,batch,tokens,kv,group,capacity,lengths,causal", PROMPTS)
+def test_every_kernel_for_prompts(hb, rows, batch, tokens, kv, group, capacity, lengths, causal, dim, dtype):
+    print(f"[prompt] {rows} rows, {dtype} b{batch} t{tokens} h{kv}x{group} dim {dim} cap {capacity} lengths {lengths}", flush=True)
+    gen = _gen(dim + tokens)
+    cache, k, v = _filled(hb, gen, batch, kv, capacity, dim, lengths)
+    q = _randn(gen, (batch, tokens, kv * group, dim), dtype)
+    call = lambda: hb.cache_attend(cache, q, _lens(lengths), causal=causal)
+    kernel = f"cache_prompt_kernel<{-(-dim // 32)}, {[F32, BF16, F16].index(dtype)}, {rows // 32}>"
+    assert kernel in launched_kernels(call)
+    out, lse = call()
+    _check_attend(out, lse, _attend64(k, v, q, lengths, dim ** -0.5, causal), dtype, dim, capacity)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("dim", [31, 64, 90, 128, 160, 170, 224, 256])
+@pytest.mark.parametrize("batch,tokens,kv,group,capacity,lengths", [(2, 1, 2, 4, 1000, [1000, 77]), (3, 3, 2, 2, 128, [128, 2, 0]), (1, 20, 2, 1, 3000, [2977])])
+def test_every_kernel_for_few_queries(hb, batch, tokens, kv, group, capacity, lengths, dim, dtype):
+    print(f"[attend] {dtype} b{batch} t{tokens} h{kv}x{group} dim {dim} cap {capacity} lengths {lengths}", flush=True)
+    gen = _gen(dim + tokens)
+    cache, k, v = _filled(hb, gen, batch, kv, capacity, dim, lengths)
+    q = _randn(gen, (batch, tokens, kv * group, dim), dtype)
+    call = lambda: hb.cache_attend(cache, q, _lens(lengths))
+    assert f"cache_attend_kernel<{-(-dim // 32)}, {[F32, BF16, F16].index(dtype)}>" in launched_kernels(call)
+    out, lse = call()
+    want = _attend64(k, v, q, lengths, dim ** -0.5)
+    _check_attend(out, lse, want, dtype, dim, capacity)
+    w = hb.cache_weigh(cache, q, lse, _lens(lengths), torch.zeros((batch, kv, capacity), device="cuda"))
+    d = (dim + 16) * 2.0 ** -24 * want[3].max() + (64 + capacity / 32) * 2.0 ** -24 + 2.0 ** -21 * (1 + want[1][torch.isfinite(want[1])].abs().max())
+    assert ((w.double() - want[4]).abs() <= (2 * d + tokens * group * 2.0 ** -24) * want[4]).all()
+
+
+PRODUCTS = [
+    # the kernel (and that for its slices), M, N, K
+    ("gemm_rows_few_kernel<1, 2, 16, {t}, true>", 1, 5120, 300), ("gemm_rows_few_kernel<1, 2, 16, {t}, true>", 2, 77, 16384),
+    ("gemm_rows_few_kernel<1, 4, 8, {t}, true>", 1, 5121, 1000), ("gemm_rows_few_kernel<1, 4, 8, {t}, true>", 1, 20001, 129),
+    ("gemm_rows_few_kernel<1, 4, 8, {t}, true>", 2, 16384, 513),
+    ("gemm_rows_few_kernel<1, 8, 4, {t}, false>", 2, 16385, 200), ("gemm_rows_few_kernel<1, 8, 4, {t}, false>", 16, 8193, 1100),
+    ("gemm_rows_few_kernel<1, 8, 4, {t}, false>", 1, 8200, 33000), ("gemm_rows_few_kernel<1, 4, 8, {t}, false>", 16, 8192, 70),
+    ("gemm_rows_few_kernel<1, 4, 8, {t}, false>", 3, 50, 5000), ("gemm_rows_few_kernel<2, 1, 16, {t}, false>", 32, 130, 4096),
+    ("gemm_rows_few_kernel<2, 1, 16, {t}, false>", 17, 4099, 1000),
+    ("gemm_i8_wide_kernel<2, 64, 4, {o}, ", 96, 88, 33), ("gemm_i8_wide_kernel<2, 64, 4, {o}, +rows_sum_kernel<{o}>", 72, 65, 1962),
+    ("gemm_i8_wide_kernel<2, 64, 4, {o}, +rows_sum_kernel<{o}>", 65, 64, 4000), ("gemm_i8_wide_kernel<2, 64, 4, {o}, +rows_sum_kernel<{o}>", 130, 70, 40001),
+    ("gemm_i8_wide_kernel<2, 64, 4, {o}, +rows_sum_kernel<{o}>", 70, 66, 133144),
+    ("gemm_i8_wide_kernel<2, 128, 4, {o}, +rows_sum_kernel<{o}>", 130, 499, 133144), ("gemm_i8_wide_kernel<2, 128, 4, {o}, ", 900, 941, 3155),
+    ("gemm_i8_wide_kernel<2, 128, 2, {o}, ", 2446, 1571, 1155), ("gemm_i8_wide_kernel<2, 128, 2, {o}, +rows_sum_kernel<{o}>", 1289, 927, 5642),
+    ("gemm_i8_wide_kernel<3, 64, 4, {o}, ", 2187, 3884, 33), ("gemm_i8_wide_kernel<3, 128, 3, {o}, ", 2506, 3091, 1025),
+    ("gemm_i8_wide_kernel<4, 64, 4, {o}, ", 2973, 3586, 2454), ("gemm_i8_wide_kernel<4, 128, 2, {o}, ", 4495, 3351, 133),
+    ("gemm_i8_wide_kernel<4, 128, 2, {o}, ", 4608, 3328, 260),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("kernel,m,n,k", PRODUCTS)
+def test_every_kernel_for_products(hb, kernel, m, n, k, dtype):
+    """The int32 sum is exact; two scales and a bias are three FP32 roundings, the output one of its type."""
+    print(f"[product] {kernel} {dtype} {m}x{n}x{k}", flush=True)
+    gen, t = _gen(m + n + k), [F32, BF16, F16].index(dtype)
+    x, w = _randn(gen, (m, k), dtype, 2), hb.quant_rows(_randn(gen, (n, k)))
+    bias = torch.randn(n, generator=gen, device="cuda")
+    names = launched_kernels(lambda: hb.linear_i8(x, w, bias=bias))
+    for part in kernel.format(t=t, o=t + 1).split("+"):
+        assert any(name.startswith(part) for name in names), names
+    a = hb.quant_rows(x)
+    sums = a.codes[:, :k].double() @ w.codes[:, :k].double().t().contiguous()
+    product = sums * a.scales.double().unsqueeze(1) * w.scales.double()
+    for b, offset, pitch in ((bias, 0, n), (None, 0, n + n % 2 + 2), (bias, 1, n + n % 2 + 4), (None, 2, n + 1 - n % 2)):
+        exact = product if b is None else product + b.double()
+        tol = U[dtype] * exact.abs() + 2.0 ** -22 * (product.abs() + exact.abs()) + (2.0 ** -24 if dtype == F16 else 0)
+        room = torch.full((m * pitch + offset,), 5.0, device="cuda", dtype=dtype)
+        y = room[offset:].view(m, pitch)[:, :n]
+        assert hb.linear_i8(x, w, bias=b, out=y) is y
+        assert ((y.double() - exact).abs() <= tol).all()
+        y.fill_(5.0)
+        assert (room == 5).all(), "bytes around the output"
+
+
+# ------------------------------------------------------------------------------------------------------------- the layer
+@pytest.mark.parametrize("batch,heads,kv_heads,dim,prompt,steps", [(5, 8, 2, 64, 200, 70), (1, 6, 6, 80, 256, 20), (3, 4, 1, 128, 37, 10)])
+def test_the_layer_of_the_example_on_the_values_its_cache_holds(hb, batch, heads, kv_heads, dim, prompt, steps):
+    """examples/serve_layer.py against 64 bits whose operands are what the layer holds: 8-bit weights and tokens, the cache's values.
+    Tolerances (of the norm): q and the attention's output are rounded to bf16, 0.0011 each in the RMS; that moves a twentieth of the
+    output's 8-bit codes (a step is 0.024 of a standard deviation) by one, 0.0054; 0.02 leaves a factor of three.  A token too many or
+    missing, of 256, is 0.06.  New tokens in the cache are the 4-bit values of the layer's own k and v but where the bf16 rounding of the
+    product moves a 4-bit code, one in a hundred by a quarter of a standard deviation: 0.03; the wrong slot is 1.4."""
+    from examples.serve_layer import Layer
+    from tests import serve_ref
+    print(f"[layer] b{batch} h{heads}/{kv_heads} dim {dim} prompt {prompt} steps {steps}", flush=True)
+    gen, features, capacity = _gen(15), 384, 256
+    w_qkv, w_out = (_randn(gen, shape, BF16, 0) / math.sqrt(shape[1]) for shape in (((heads + 2 * kv_heads) * dim, features), (features, heads * dim)))
+    layer = Layer(w_qkv, w_out, batch, heads, kv_heads, dim, capacity)
+    values = lambda c: c.codes[:, :c.cols].double() * c.scales.double().unsqueeze(1)
+    product = lambda x, w: values(hb.quant_rows(x)) @ values(w).t().contiguous()
+    relative = lambda got, want: ((got.double() - want).norm() / want.norm()).item()
+    lengths = [max(1, prompt - 30 * b) for b in range(batch)]
+    counts = list(lengths)
+    history = [[torch.zeros((kv_heads, 0, dim), dtype=torch.float64, device="cuda") for _ in range(2)] for _ in range(batch)]
+    for step in range(steps + 1):
+        if max(lengths) + (step > 0) > capacity:
+            kept = layer.shrink(64, 16)
+            for b, n in enumerate(lengths):
+                m = min(n, 64)
+                assert (kept[b, :, m:] == -1).all() and (n <= 64 or (kept[b, :, 48:] == torch.arange(n - 16, n, device="cuda")).all())
+                at = kept[b, :, :m].long().unsqueeze(2).expand(-1, -1, dim)
+                history[b] = [t.gather(1, at) for t in history[b]]
+                lengths[b] = m
+        tokens = max(counts) if step == 0 else 1
+        if step:
+            counts, lengths = [1] * batch, [n + 1 for n in lengths]
+        x = _randn(gen, (batch, tokens, features), BF16, 0)
+        y = layer.step(x, torch.tensor(counts, dtype=torch.int32, device="cuda"))
+        assert layer.lengths.tolist() == lengths
+        k, v = (t.double() for t in hb.cache_read(layer.cache, layer.lengths))
+        qkv = product(x.view(batch * tokens, features), layer.w_qkv).to(BF16).view(batch, tokens, -1, dim)
+        for b, n in enumerate(counts):
+            for i, (held, h0) in enumerate(((k, heads), (v, heads + kv_heads))):
+                new = torch.from_numpy(serve_ref.cached(qkv[b, tokens - n:, h0:h0 + kv_heads].double().cpu().numpy())).cuda().transpose(0, 1)
+                history[b][i] = torch.cat([history[b][i], new], dim=1)
+                assert relative(held[b, :, :lengths[b]], history[b][i]) < 0.03
+        out = _attend64(k, v, qkv[:, :, :heads], lengths, dim ** -0.5)[0].to(BF16)
+        want = product(out.view(batch * tokens, heads * dim), layer.w_out).view(batch, tokens, features)
+        for b, n in enumerate(counts):
+            assert relative(y[b, tokens - n:], want[b, tokens - n:]) < 0.02, (step, b)
