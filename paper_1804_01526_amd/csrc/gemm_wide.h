@@ -370,7 +370,7 @@ __device__ __forceinline__ void wide_sum(const WideParams &p) {
         *dst = p.beta ? *dst + val : val;
     }
 }
-__global__ __launch_bounds__(256) void wide_sum_kernel(const WideParams p) { wide_sum<kWideExponents>(p); }
+[[maybe_unused]] __global__ __launch_bounds__(256) void wide_sum_kernel(const WideParams p) { wide_sum<kWideExponents>(p); }
 template <int OUT>
 __global__ __launch_bounds__(256) void rows_sum_kernel(const WideParams p) { wide_sum<OUT>(p); }
 
@@ -378,7 +378,9 @@ template <int T, int K, int RING, int OUT>
 int launch_wide_t(WideParams p, bool stream, hipStream_t s) {
     static std::atomic<bool> configured[2];
     constexpr int lds_bytes = Wide<T, K, RING>::kLds;
-    void (*const kernel)(WideParams) = stream ? &gemm_i8_wide_kernel<T, K, RING, OUT, true> : &gemm_i8_wide_kernel<T, K, RING, OUT, false>;
+    constexpr bool kStreams = OUT == kWideExponents || OUT == kWideF32;      // (16-bit outputs leave by ordinary stores)
+    stream = stream && kStreams;
+    void (*const kernel)(WideParams) = stream ? &gemm_i8_wide_kernel<T, K, RING, OUT, kStreams> : &gemm_i8_wide_kernel<T, K, RING, OUT, false>;
     if (allow_dynamic_lds(configured[stream], reinterpret_cast<const void *>(kernel), lds_bytes) != HBFP_OK) return HBFP_ERR_LAUNCH;
     p.nstage *= 128 / K;
     p.stages_per_split *= 128 / K;

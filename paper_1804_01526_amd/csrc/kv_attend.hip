@@ -301,11 +301,11 @@ int launch_join(const SplitParams &p, hipStream_t s) {
 // different length need more of them, so that the longest does not hold the last workgroups alone.  us with 1024, 1536, 2048, 4096 and
 // 8192 workgroups: 32 conversations of 128 to 8192 tokens 40, 31, 27, 30, 38, 16 of them 24, 20, 23, 25, 36; one of 200001 tokens 36, 35,
 // 39, 42, 58, and joining its chunks 9.4, 10.1, 10.6, 14.8, 23.0
-SplitParams split_of(const AttendArgs &a, int dtype) {
+SplitParams split_of(const AttendArgs &a) {
     SplitParams p = {};
     p.a = a;
     p.rows = a.tokens * a.group;
-    const bool prompt = cache_prompt_ok(a, dtype);
+    const bool prompt = cache_prompt_ok(a);
     p.tile_rows = prompt ? (int32_t)cache_prompt_rows(a) : 16;
     p.tiles = (int32_t)ceil_div(p.rows, p.tile_rows);
     p.scale2 = a.scale * kLog2e;
@@ -467,19 +467,19 @@ int launch_weigh_of(const WeighParams &p, hipStream_t s) {
 
 }  // namespace
 
-size_t cache_attend_workspace(const AttendArgs &a, int dtype) {
-    return split_floats(split_of(a, dtype)) * 4;
+size_t cache_attend_workspace(const AttendArgs &a) {
+    return split_floats(split_of(a)) * 4;
 }
 
 int launch_cache_attend(const AttendArgs &a, int dtype, hipStream_t s) {
-    SplitParams p = split_of(a, dtype);
+    SplitParams p = split_of(a);
     const int64_t heads = (int64_t)a.c.batch * a.c.heads;
     const int64_t wgs = heads * p.tiles * p.chunks, rows = heads * p.rows;
     if (wgs > 0x7fffffff || rows > 0x7fffffff) return HBFP_ERR_ARG;
     p.wgs = (uint32_t)wgs;
     p.o = a.ws;
     p.ml = a.ws ? a.ws + heads * p.chunks * p.rows * 32 * a.c.nblk : nullptr;
-    int rc = cache_prompt_ok(a, dtype) ? launch_cache_prompt(p, dtype, s)
+    int rc = cache_prompt_ok(a) ? launch_cache_prompt(p, dtype, s)
              : dtype == HBFP_F32 ? launch_split_of<HBFP_F32>(p, s) : dtype == HBFP_BF16 ? launch_split_of<HBFP_BF16>(p, s) : launch_split_of<HBFP_F16>(p, s);
     if (rc != HBFP_OK || p.chunks == 1) return rc;
     return dtype == HBFP_F32 ? launch_join<HBFP_F32>(p, s) : dtype == HBFP_BF16 ? launch_join<HBFP_BF16>(p, s) : launch_join<HBFP_F16>(p, s);

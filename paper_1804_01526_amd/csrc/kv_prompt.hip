@@ -364,8 +364,7 @@ int launch_prompt_of(const SplitParams &p, hipStream_t s) {
 
 // Rows from which the tiles of this kernel are ahead of tiles of 16 (below, most of a tile of 64 would be empty), and their height:
 // tall where the chip is full either way, because a tile of keys is converted once for all rows of a workgroup
-bool cache_prompt_ok(const AttendArgs &a, int dtype) {
-    (void)dtype;
+bool cache_prompt_ok(const AttendArgs &a) {
     return a.c.nblk <= 4 && (int64_t)a.tokens * a.group > 48;
 }
 int64_t cache_prompt_rows(const AttendArgs &a) {

@@ -21,7 +21,6 @@ struct AppendParams {
 };
 
 // eight mantissas as nibbles (low: 0..3, high: 4..7, one byte each pair) and the exponent byte of the block
-template <int DT>
 __device__ __forceinline__ uint32_t convert8(const float *x, uint32_t &Eb) {
     uint32_t amax = 0;
 #pragma unroll
@@ -69,7 +68,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendParams p)
     load8<DT>(p.k.data, b * p.k.sb + t * p.k.st + h * p.k.sh + d0, n, xk);
     load8<DT>(p.v.data, b * p.v.sb + t * p.v.st + h * p.v.sh + d0, n, xv);
     uint32_t ek, ev;
-    const uint32_t wk = convert8<DT>(xk, ek), wv = convert8<DT>(xv, ev);
+    const uint32_t wk = convert8(xk, ek), wv = convert8(xv, ev);
     // an Inf or a NaN in a value is marked in the key's exponent, which makes the score of whoever sees the token NaN: the kernels
     // then never meet a value that is not finite, and a weight of 0 silences any value
     ek = ev == 255u ? 255u : ek;

@@ -43,10 +43,10 @@ int launch_cache_read(const CacheView &c, const int32_t *lengths, int dtype, voi
 int launch_cache_evict(const CacheView &src, const float *w, int64_t ld, const int32_t *lengths, int64_t keep, int64_t recent,
                        const CacheView &dst, float *w_out, int64_t ld_out, int32_t *kept, int32_t *lengths_out, hipStream_t s);
 // kv_attend.hip
-size_t cache_attend_workspace(const AttendArgs &a, int dtype);
+size_t cache_attend_workspace(const AttendArgs &a);
 int launch_cache_attend(const AttendArgs &a, int dtype, hipStream_t s);
 // kv_prompt.hip: many rows a key head
-bool cache_prompt_ok(const AttendArgs &a, int dtype);
+bool cache_prompt_ok(const AttendArgs &a);
 int64_t cache_prompt_rows(const AttendArgs &a);
 int launch_cache_prompt(const SplitParams &p, int dtype, hipStream_t s);
 struct WeighArgs {

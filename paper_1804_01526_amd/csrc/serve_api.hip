@@ -141,7 +141,7 @@ int hbfp_cache_attend_workspace(const hbfp_cache *cache, int64_t tokens, int64_t
     AttendArgs a;
     const int rc = attend_args(&plan, tokens, heads, longest, &a);
     if (rc != HBFP_OK) return rc;
-    *bytes = align256(cache_attend_workspace(a, dtype));
+    *bytes = align256(cache_attend_workspace(a));
     return HBFP_OK;
 }
 
@@ -162,7 +162,7 @@ int hbfp_cache_attend(const hbfp_cache *cache, const hbfp_heads *q, int64_t toke
     a.lse = lse;
     a.causal = causal;
     a.scale = scale;
-    const size_t need = align256(cache_attend_workspace(a, q->dtype));
+    const size_t need = align256(cache_attend_workspace(a));
     if (need && (!workspace || ws_bytes < need || ((uintptr_t)workspace & 255))) return HBFP_ERR_WORKSPACE;
     a.ws = need ? (float *)workspace : nullptr;
     return launch_cache_attend(a, q->dtype, (hipStream_t)stream);

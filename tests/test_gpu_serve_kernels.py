@@ -310,6 +310,13 @@ def test_every_kernel_for_products(hb, kernel, m, n, k, dtype):
         assert (room == 5).all(), "bytes around the output"
 
 
+@pytest.mark.parametrize("dtype,stream", [(F32, "true"), (BF16, "false"), (F16, "false")])
+def test_products_of_16_bits_have_one_kind_of_store(hb, dtype, stream):
+    gen = _gen(16)
+    x, w = _randn(gen, (900, 3155), dtype), hb.quant_rows(_randn(gen, (941, 3155)))
+    assert f"gemm_i8_wide_kernel<2, 128, 4, {[F32, BF16, F16].index(dtype) + 1}, {stream}>" in launched_kernels(lambda: hb.linear_i8(x, w))
+
+
 # ------------------------------------------------------------------------------------------------------------- the layer
 @pytest.mark.parametrize("batch,heads,kv_heads,dim,prompt,steps", [(5, 8, 2, 64, 200, 70), (1, 6, 6, 80, 256, 20), (3, 4, 1, 128, 37, 10)])
 def test_the_layer_of_the_example_on_the_values_its_cache_holds(hb, batch, heads, kv_heads, dim, prompt, steps):
