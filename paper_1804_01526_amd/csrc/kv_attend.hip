@@ -297,10 +297,13 @@ int launch_join(const SplitParams &p, hipStream_t s) {
     return launch_status();
 }
 
-// Chunks of keys: enough workgroups to fill the chip several times over, none shorter than a step of its four waves.  Conversations of
-// different length need more of them, so that the longest does not hold the last workgroups alone.  us with 1024, 1536, 2048, 4096 and
-// 8192 workgroups: 32 conversations of 128 to 8192 tokens 40, 31, 27, 30, 38, 16 of them 24, 20, 23, 25, 36; one of 200001 tokens 36, 35,
-// 39, 42, 58, and joining its chunks 9.4, 10.1, 10.6, 14.8, 23.0
+// Chunks of keys: enough workgroups to fill the chip several times over, none shorter than a step of its four waves.  Several
+// conversations may differ in length, which the host does not know: they get twice as many, so that the longest does not hold the last
+// workgroups alone, and equal ones pay for that.  us, joining included, with 1024, 1536, 2048 and 4096 of them, 128 dimensions.  One of 200001
+// tokens, 16 heads (4 of keys) 43.4, 42.3, 45.8, 53.7, 32 heads (8 of keys) over 8192 12.2, 12.3, 12.3, 12.3.  Different lengths, 32 heads: 16
+// of 128 to 8192 31.6, 27.1, 31.9, 33.3, 32 of them 52.2, 40.1, 40.1, 41.9, another 32 (a whole step from cold caches) 1536 46.4, 2048
+// 43.0.  Equal ones: 2 of 100000, 16 heads 40.2, 40.1, 43.0, 48.4; 32 heads, 8 of 8192 26.5, 29.9, 30.0, 40.0, 32 of 4096 40.4, 40.8,
+// 42.9, 51.2
 SplitParams split_of(const AttendArgs &a) {
     SplitParams p = {};
     p.a = a;
