@@ -7,7 +7,7 @@
 namespace hbfp {
 namespace {
 
-// ---- rows -> codes.  A workgroup has one row: its largest magnitude, then its codes.  Bound by memory: 4096 x 4096 bf16 in 16 us, 3.0 TB/s.
+// ---- rows -> codes.  A workgroup has one row: its largest magnitude, then its codes.  Bound by memory: 4096 x 4096 bf16 in 16.4 us, 3.1 TB/s.
 struct QuantParams {
     const void *src;
     int8_t *codes;

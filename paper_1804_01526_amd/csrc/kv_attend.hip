@@ -135,9 +135,10 @@ __device__ __forceinline__ void attend_step(const StepWords<NB, KS> &r, int key0
         }
 }
 
-// Bound by bytes on their way and by the vector instructions that turn nibbles into numbers: with four queries a head only a quarter of
-// every tile of 16 is real, and the conversion is the same as for all.  16 heads (4 of keys) of 128 over 200001 tokens: 109 MB in
-// 37 us, 3.0 TB/s; 32 conversations of 128 to 8192 tokens, 32 heads (8 of keys): 62 MB in 30 us, 2.1 TB/s (weights as one piece: 27).
+// Bound by the vector instructions that turn nibbles and weights into numbers, 70 to 80 % of a busy compute unit's cycles: with four
+// queries a head only a quarter of every tile of 16 is real, and the conversion is the same as for all.  16 heads (4 of keys) of 128 over
+// 200001 tokens, FP16: 109 MB in 37 us, 3.0 TB/s; 32 conversations of 128 to 8192 tokens, 32 heads (8 of keys), bf16: 62 MB in 34 us,
+// 1.8 TB/s (weights as one piece: 30), the compute units busy half of the time because lengths differ.
 // A workgroup's four waves take the steps of a chunk in turn and join their results in LDS; with several chunks the joined
 // ones go to the workspace, and cache_join_kernel joins those.
 template <int NB, int DT>
@@ -349,7 +350,7 @@ int launch_split_of(const SplitParams &p, hipStream_t s) {
 
 // ---- accumulated weights.  A wave turns 64 keys into bf16 numbers once and meets every query of the key head with them; a
 // lane's sums over its query columns are exchanged over the 16 lanes at the end.  A wave walks over kWeighGroups such groups, the
-// words of the next on their way; queries that fit one tile stay in registers.  Bound by latency and conversion as the attention: 16
+// words of the next on their way; queries that fit one tile stay in registers.  Bound by latency (half of the waves' time waits for memory): 16
 // conversations of 128 to 8192 tokens, 32 heads (8 of keys) of 128, 45 MB in 26 us, 1.8 TB/s (a group a wave: 48 us).
 constexpr int kWeighGroups = 4;
 struct WeighParams {

@@ -4,10 +4,10 @@
 // values are turned into bf16 numbers once, exactly, by all its waves together, into LDS: keys as they are, values transposed,
 // in the order in which the scores' register layout presents keys.  Then S^T = K Q^T and O^T += V^T P^T as in the kernel for
 // few queries, on the 32 x 32 x 16 matrix instruction: a lane holds one query, and its softmax needs one exchange with the lane
-// 32 away.  Weights enter the second product as two pieces (bf16, FP16), so it costs twice its operations.  Two prompts of 2048 tokens
-// over 4096, 32 heads (8 of keys) of 128, causal, bf16: 206 Gflop, 309 on the matrix core, in 296 us (one piece: 246), 1.04 PFLOP/s
-// of the 1.2 that a large bf16 product reaches; three of 501 tokens, 6 heads (2 of keys) of 96, FP16: 22 us and 4.7 for joining the
-// chunks.
+// 32 away.  Weights enter the second product as two pieces (bf16, FP16), so it costs twice its operations, and the matrix core
+// bounds large prompts.  Two of 2048 tokens over 4096, 32 heads (8 of keys) of 128, causal, bf16: 206 Gflop, 309 on the matrix core, in
+// 287 to 300 us (one piece: 225 to 240), 1.03 to 1.08 PFLOP/s of the 1.2 that a large bf16 product reaches; three of 501 tokens, 6 heads
+// (2 of keys) of 96, FP16: 22 us, that of the longest of few workgroups, and 4.8 for joining the chunks.
 #include "kv_cache.h"
 
 namespace hbfp {
