@@ -828,6 +828,118 @@ int hbfp_linear_i8_workspace(int64_t M, int64_t N, int64_t K, size_t *bytes);
 int hbfp_linear_i8(const void *x, int dtype, int64_t M, int64_t K, int64_t ldx, const int8_t *b, const float *b_scales,
                    const float *bias, int64_t N, void *y, int64_t ldy, void *workspace, size_t ws_bytes, void *stream);
 
+/*
+ * ---- Microscaled 4-bit floating point: conversion and products
+ *
+ * The floating sibling of the 4-bit mantissas above: blocks of 32 values along the contraction share a power of two, and a value is
+ * one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign, times it (two exponent bits, one mantissa bit; 4.25 bits a value with the block's
+ * byte).  The matrix instruction takes such blocks as they are stored.
+ *   scale byte  s = 0..254 stands for 2^(s - 127).  With Eb the IEEE-754 biased exponent of the block's largest magnitude, raised by
+ *               one where that magnitude would round to 8 units (to nearest: its significand is at least 1.75) or exceeds 6 units
+ *               (stochastic: above 1.5, so that nothing is cut off and the rounding keeps the mean): s = max(min(Eb, 254) - 2, 0).
+ *               255: the block holds an Inf or a NaN; its codes are 0 and every product with it is NaN.
+ *   code        bit 3 the sign, bits 0..2 the index of the magnitude in the list above.  HBFP_RNE: the nearest, ties to the even
+ *               index.  HBFP_STOCHASTIC: with `step` the distance of the list's members around |x| (0.5, 1 or 2 units) and h the
+ *               random word of the element (hash above, idx = r * cols + c of the source, whatever the axis),
+ *               floor(|x| / step + h / 2^32) steps.  A magnitude above 6 units (from 1.75 * 2^127 on alone) becomes 6.
+ * hbfp_mx4 is an operand of `rows` rows and a contraction of `kdim`.  hbfp_mx4_plan fills everything but the two pointers; the
+ * caller sets those (device, 16-byte aligned).  The contraction is cut into groups of 256:
+ *   codes    [groups][rows][128]       byte j of a group's row: elements 256 group + 2 j (low nibble) and 2 j + 1 (high nibble)
+ *   scales   [groups][scale_rows][8]   byte b of a group's row: elements 256 group + 32 b ...; scale_rows = rows rounded up to 16
+ * Elements from kdim to the end of the last group are stored as 0 (their blocks' bytes as 0); scale rows from `rows` on may hold
+ * anything.
+ */
+typedef struct hbfp_mx4 {
+    uint8_t *codes;              /* device, code_bytes, 16-byte aligned */
+    uint8_t *scales;             /* device, scale_bytes, 16-byte aligned */
+    int64_t rows, kdim;
+    int64_t groups, scale_rows;
+    uint64_t code_bytes, scale_bytes;
+} hbfp_mx4;
+
+/* hbfp_mx4_plan (host only).  Errors: HBFP_ERR_ARG (null, sizes <= 0 or from 2^31 on). */
+int hbfp_mx4_plan(int64_t rows, int64_t kdim, hbfp_mx4 *out);
+
+/*
+ * hbfp_quant_mx4: converts a matrix [rows][ld] of HBFP_F32, HBFP_BF16 or HBFP_F16, read once, into one or both operands of it:
+ *   along   planned for (rows, cols): the contraction runs along the source's rows (weights [out][in] and tokens of a forward product)
+ *   down    planned for (cols, rows): it runs down the columns (the operands of the two gradients' products)
+ * Either may be NULL.  Outputs may not overlap the source or each other.
+ * hbfp_read_mx4: the values an operand holds, dst [rows][ld] for ld >= kdim, in HBFP_F32 or HBFP_BF16 (exact in both); NaN in blocks whose byte is 255.
+ * Errors: HBFP_ERR_ARG, HBFP_ERR_FORMAT (dtype, rounding), HBFP_ERR_LAYOUT (operand differs from its plan), HBFP_ERR_LAUNCH.
+ */
+int hbfp_quant_mx4(const void *src, int dtype, int64_t rows, int64_t cols, int64_t ld, int rounding, uint64_t seed,
+                   const hbfp_mx4 *along, const hbfp_mx4 *down, void *stream);
+int hbfp_read_mx4(const hbfp_mx4 *t, int dtype, void *dst, int64_t ld, void *stream);
+
+/*
+ * hbfp_gemm_mx4: Y[m][n] = sum_k a[m][k] b[n][k] + bias[n] of the values the operands hold: blocks of 32 exactly, their sums in FP32,
+ * Y rounded once to its type.  a: M = a->rows rows, b: N = b->rows rows, equal kdim.  bias: FP32 [N] or NULL.  y: [M][ldy], ldy >= N.
+ * The three products of a linear layer y = x w^T, with x [tokens][in], w [out][in] and dy [tokens][out]:
+ *   y = x along . w along;   dx = dy along . w down;   dw = dy down . x down.
+ * hbfp_linear_mx4: hbfp_quant_mx4 of x (to nearest, along its rows) and the product in one call; Y has x's type.  Rows of y may not
+ * overlap rows of x (refused with HBFP_ERR_ARG where the call reads x and writes y in one launch); both may be columns of one matrix.
+ * workspace: the matching _workspace bytes, 256-byte aligned.
+ * Errors: HBFP_ERR_ARG, HBFP_ERR_FORMAT (dtype), HBFP_ERR_LAYOUT (operand differs from its plan, or the two do not fit each other),
+ * HBFP_ERR_WORKSPACE, HBFP_ERR_LAUNCH.
+ */
+int hbfp_gemm_mx4_workspace(int64_t M, int64_t N, int64_t K, size_t *bytes);
+int hbfp_gemm_mx4(const hbfp_mx4 *a, const hbfp_mx4 *b, const float *bias, void *y, int dtype, int64_t ldy, void *workspace,
+                  size_t ws_bytes, void *stream);
+int hbfp_linear_mx4_workspace(int64_t M, int64_t N, int64_t K, size_t *bytes);
+int hbfp_linear_mx4(const void *x, int dtype, int64_t M, int64_t ldx, const hbfp_mx4 *w, const float *bias, void *y, int64_t ldy,
+                    void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * ---- The norm in front of a quantised product
+ *
+ * Root-mean-square norm of rows, with the residual's addition before it and the conversion of its rows after it:
+ *   sum  = x + residual, FP32, rounded once to the type (residual NULL: sum = x)
+ *   rstd = 1 / sqrt(mean over the row of sum^2 + eps)
+ *   n    = sum * rstd * weight, in 64 bits, rounded once to FP32 (weight: FP32 [cols] or NULL for ones)
+ * hbfp_norm_i8 delivers n as hbfp_quant_rows converts it (codes, scales: the operand of hbfp_gemm_rows), hbfp_norm_mx4 as
+ * hbfp_quant_mx4 does, to nearest and along the rows.  Up to the rounding to FP32 everything is held in 64 bits, so that codes do not
+ * depend on the order of a sum.
+ *   x, residual, sum, values   [rows] rows of `cols`, of one type, with leading dimensions of their own
+ *   sum      receives the sum (NULL: it is not stored); may be x or residual, with the same leading dimension
+ *   rstd     FP32 [rows] or NULL: what hbfp_norm_grad needs
+ *   values   NULL, or receives the values that the codes stand for, rounded to the type
+ *   eps      finite, above 0
+ * Otherwise outputs may not overlap inputs or each other (x, residual, sum and values may be columns of one matrix).  A row that holds
+ * an Inf or a NaN gets an Inf or NaN as its scale, or as that of at least one block, so that what is multiplied with it is NaN or Inf.
+ * Errors: HBFP_ERR_ARG, HBFP_ERR_FORMAT (dtype), HBFP_ERR_LAYOUT (out is not the plan of (rows, cols)), HBFP_ERR_LAUNCH.
+ */
+typedef struct hbfp_norm {
+    const void *x;               /* device */
+    const void *residual;        /* device or NULL */
+    const float *weight;         /* device FP32 [cols] or NULL */
+    void *sum;                   /* device or NULL */
+    void *values;                /* device or NULL */
+    float *rstd;                 /* device FP32 [rows] or NULL */
+    int64_t rows, cols;
+    int64_t ldx, ld_residual, ld_sum, ld_values;   /* elements, >= cols where the pointer is not NULL */
+    int32_t dtype;               /* HBFP_F32, HBFP_BF16 or HBFP_F16 */
+    float eps;
+} hbfp_norm;
+int hbfp_norm_i8(const hbfp_norm *norm, int8_t *codes, float *scales, void *stream);
+int hbfp_norm_mx4(const hbfp_norm *norm, const hbfp_mx4 *out, void *stream);
+
+/*
+ * hbfp_norm_grad: the gradient of the norm above, the conversion counted as the identity.  With g the gradient of n and g_sum that
+ * which reaches `sum` by other ways (NULL: none):
+ *   dx      = g_sum + rstd * (g * weight - sum * rstd^2 * mean over the row of (g * weight * sum)),  rounded once to the type: the
+ *             gradient of x, and of the residual
+ *   dweight = sum over the rows of g * sum * rstd, FP32 [cols]; overwritten (NULL: not computed)
+ * Statistics and sums are FP32 and taken in an order that depends on the sizes alone.  sum, rstd: what the forward call stored.
+ * dx may be g or g_sum, with the same leading dimension.
+ * workspace: hbfp_norm_grad_workspace bytes, 256-byte aligned; none without dweight.
+ * Errors: HBFP_ERR_ARG, HBFP_ERR_FORMAT, HBFP_ERR_WORKSPACE, HBFP_ERR_LAUNCH.
+ */
+int hbfp_norm_grad_workspace(int64_t rows, int64_t cols, size_t *bytes);
+int hbfp_norm_grad(const void *g, int64_t ldg, const void *sum, int64_t ld_sum, const float *rstd, const float *weight, const void *g_sum,
+                   int64_t ld_g_sum, int dtype, int64_t rows, int64_t cols, void *dx, int64_t ldx, float *dweight, void *workspace,
+                   size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,483 @@
+// Products of microscaled 4-bit operands:
+//     y[m][n] = sum over blocks of 32 of 2^(sa + sb - 254) * (sum of the block's products) + bias[n]
+// on v_mfma_scale_f32_*_f8f6f4 with both operands in 4 bits: a lane hands the instruction one block, 32 codes in 16 bytes as they
+// are stored, and its scale byte, and the instruction multiplies, scales and accumulates in FP32.
+#include "gemm_wide.h"
+#include "mx4.h"
+
+namespace hbfp {
+namespace {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+
+// the builtin takes eight registers an operand and drops the last four for this format
+__device__ __forceinline__ v8i four_bit(const v4i &x) { return v8i{x[0], x[1], x[2], x[3], 0, 0, 0, 0}; }
+
+// ---- many tokens: tiles of 64 T x 64 T.  The frame is that of the int8 kernel for one exponent per row (gemm_wide.h): four waves of
+// 32 T x 32 T, so that a pair of matrix instructions needs one 16-byte LDS read a lane; operands copied global -> LDS asynchronously
+// into a ring of stages; fragments read a k-step ahead, between the matrix instructions; a ring buffer handed over in the stage's
+// last k-step.  A stage is one group of 256 k: 128 bytes of codes a row, and 8 scale bytes.  Lanes 0..31 of a fragment have the
+// group's first four blocks, lanes 32..63 the others, so that a row's four bytes are one word of a lane for the whole stage and a
+// k-step picks its byte in the instruction.
+struct Mx4Params {
+    Mx4Product q;
+    float *partial;              // split along k: FP32 sums [splits][M][N]
+    int32_t groups, splits, groups_per_split;
+    int32_t tiles_m, tiles_n;
+};
+template <int T, int RING>
+struct Mx4Tile {
+    static constexpr int kRows = 64 * T;
+    static constexpr int kOperand = kRows * 128, kCodes = 2 * kOperand;
+    static constexpr int kScales = 2 * kRows * 8;          // T pieces of 1 KB
+    static constexpr int kStage = kCodes + kScales;
+    static constexpr int kLds = RING * kStage;
+    static constexpr int kCopies = kCodes / 1024 / 4;      // of codes per wave and stage; and one of scales
+    static __device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
+};
+
+template <int T, int RING, int OUT, bool STREAM>
+__global__ __launch_bounds__(256, T == 4 ? 1 : 2) void gemm_mx4_kernel(const Mx4Params p) {
+    typedef Mx4Tile<T, RING> W;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const Mx4Product &q = p.q;
+    int tm, tn, split = blockIdx.y;
+    if (p.splits >= 8 ? !tile_and_split_of_workgroup(blockIdx.x, p.tiles_m, p.tiles_n, p.splits, tm, tn, split)
+                      : !tile_of_workgroup(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn))
+        return;                                                                 // whole workgroup, before any barrier
+    const int st_begin = split * p.groups_per_split;
+    const int nstage = p.groups - st_begin < p.groups_per_split ? p.groups - st_begin : p.groups_per_split;   // at least 1
+
+    const int t = threadIdx.x, lane = t & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int wm = wave & 1, wn = wave >> 1;
+    const int l32 = lane & 31, lh = lane >> 5;
+    const int64_t M = q.a.rows, N = q.b.rows;
+    const int64_t row0 = (int64_t)tm * W::kRows, col0 = (int64_t)tn * W::kRows;
+
+    // ---- copies: piece c of a stage's codes is 1 KB, 8 rows; the first half are pieces of A, the others of B; wave w moves pieces w,
+    // w + 4, ...  A lane copies 16 bytes: LDS chunk lane % 8 of its row, which holds source chunk (lane % 8) ^ swizzle(row).  Rows past the
+    // edge re-read the last row (their results are never stored).
+    constexpr int kHalf = W::kCopies / 2;
+    const uint8_t *abase = q.a.codes + ((int64_t)st_begin * M + row0) * 128, *bbase = q.b.codes + ((int64_t)st_begin * N + col0) * 128;
+    uint32_t cvoff[W::kCopies];
+#pragma unroll
+    for (int i = 0; i < W::kCopies; ++i) {
+        const int r = (wave + 4 * (i < kHalf ? i : i - kHalf)) * 8 + lane / 8;
+        const int64_t lim = i < kHalf ? M - row0 : N - col0;
+        const int rr = r < lim ? r : (int)lim - 1;
+        cvoff[i] = (uint32_t)rr * 128 + (((lane & 7) ^ W::swizzle(r)) * 16);
+    }
+    // scales: rows of A, then rows of B, 8 bytes each, in T pieces of 1 KB, two rows a lane; waves past T move a piece again
+    const uint8_t *sbase;
+    int64_t sstep;
+    const int spiece = wave % T;
+    {
+        int r = spiece * 128 + 2 * lane;
+        const bool is_a = r < W::kRows;
+        r -= is_a ? 0 : W::kRows;
+        const Mx4View &v = is_a ? q.a : q.b;
+        const int64_t at = (is_a ? row0 : col0) + r, last = v.scale_rows - 2;
+        sbase = v.scales + ((int64_t)st_begin * v.scale_rows + (at < last ? at : last)) * 8;
+        sstep = v.scale_rows * 8;
+    }
+#define HBFP_MX4_COPY(i, ring_) \
+    async_copy16((i) < kHalf ? abase : bbase, cvoff[i], (uint32_t)((ring_) * W::kStage + (wave + 4 * (i)) * 1024))
+#define HBFP_MX4_COPY_LAST(ring_)                                                                            \
+    {                                                                                                       \
+        async_copy16_at(sbase, (uint32_t)((ring_) * W::kStage + W::kCodes + spiece * 1024));                \
+        sbase += sstep;                                                                                     \
+        abase += M * 128;                                                                                   \
+        bbase += N * 128;                                                                                   \
+    }
+#define HBFP_MX4_COPY_STAGE(ring_)                                                                           \
+    {                                                                                                       \
+        _Pragma("unroll") for (int i = 0; i < W::kCopies; ++i) HBFP_MX4_COPY(i, ring_);                    \
+        HBFP_MX4_COPY_LAST(ring_);                                                                          \
+    }
+
+    // ---- fragment addresses inside a stage: row tile i of A is rows 32 T wm + 32 i + l32, k-step s its chunk 4 lh + s
+    int fa[4], fb[4];
+    const int ra = 32 * T * wm + l32, rb = 32 * T * wn + l32;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        fa[s] = ra * 128 + (((4 * lh + s) ^ W::swizzle(ra)) * 16);
+        fb[s] = W::kOperand + rb * 128 + (((4 * lh + s) ^ W::swizzle(rb)) * 16);
+    }
+    const int ga = W::kCodes + ra * 8 + 4 * lh, gb = W::kCodes + (W::kRows + rb) * 8 + 4 * lh;
+
+    v16f acc[T][T];
+#pragma unroll
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+        for (int j = 0; j < T; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+
+    v4i a[2][T], b[2][T];                               // [buffer][tile]
+    int as[2][T], bs[2][T];                             // scale words of this stage and of the next
+#define HBFP_MX4_FENCE                  \
+    asm volatile("" ::: "memory");      \
+    __builtin_amdgcn_sched_barrier(0)
+#define HBFP_MX4_READ(buf, base_, s, i)                                                                        \
+    {                                                                                                         \
+        a[buf][i] = *reinterpret_cast<const v4i *>((base_) + fa[s] + (i) * 32 * 128);                         \
+        b[buf][i] = *reinterpret_cast<const v4i *>((base_) + fb[s] + (i) * 32 * 128);                         \
+    }
+#define HBFP_MX4_READ_SCALES(buf, base_, i)                                                                    \
+    {                                                                                                         \
+        as[buf][i] = *reinterpret_cast<const int *>((base_) + ga + (i) * 32 * 8);                             \
+        bs[buf][i] = *reinterpret_cast<const int *>((base_) + gb + (i) * 32 * 8);                             \
+    }
+#define HBFP_MX4_ROW(buf, s, i)                                                                                \
+    {                                                                                                         \
+        _Pragma("unroll") for (int j = 0; j < T; ++j)                                                         \
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(four_bit(a[buf][i]), four_bit(b[buf][j]), acc[i][j], 4, 4, s, \
+                                                                        as[0][i], s, bs[0][j]);               \
+    }
+    // one k-step of 64: T x T matrix instructions on buffer `buf`; after each row of them, one row tile and one column tile of the next
+    // k-step are requested into the other buffer
+#define HBFP_MX4_KSTEP(s, base_)                                                                               \
+    {                                                                                                         \
+        _Pragma("unroll") for (int i_ = 0; i_ < T; ++i_) {                                                    \
+            HBFP_MX4_ROW((s) & 1, s, i_);                                                                     \
+            HBFP_MX4_READ(1 - ((s) & 1), base_, (s) + 1, i_);                                                 \
+            HBFP_MX4_FENCE;                                                                                   \
+        }                                                                                                     \
+    }
+    // A stage is four k-steps; the fragments of its first, and its scale words, were requested during the stage before.  The hand-over,
+    // in its last: this wave has its last fragments of the stage, and its copies of the next stage have landed when only those of the
+    // AFTER stages behind it are in flight; after the barrier that holds for everybody, and the buffer takes the copies of stage st + RING
+    // (COPY).  LAST: nothing follows.
+#define HBFP_MX4_STAGE(AFTER, COPY, LAST)                                                                      \
+    {                                                                                                         \
+        const uint8_t *base = lds + ring * W::kStage;                                                         \
+        const int next = ring + 1 == RING ? 0 : ring + 1;                                                     \
+        const uint8_t *nbase = lds + next * W::kStage;                                                        \
+        HBFP_MX4_KSTEP(0, base);                                                                              \
+        HBFP_MX4_KSTEP(1, base);                                                                              \
+        HBFP_MX4_KSTEP(2, base);                                                                              \
+        _Pragma("unroll") for (int i_ = 0; i_ < T; ++i_) {                                                    \
+            HBFP_MX4_ROW(1, 3, i_);                                                                           \
+            if (!(LAST)) {                                                                                    \
+                if (i_ == 0) {                                                                                \
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((AFTER) * (W::kCopies + 1)) : "memory"); \
+                    __builtin_amdgcn_s_barrier();                                                             \
+                    asm volatile("" ::: "memory");                                                            \
+                }                                                                                             \
+                HBFP_MX4_READ(0, nbase, 0, i_);                                                               \
+                HBFP_MX4_READ_SCALES(1, nbase, i_);                                                           \
+                if (COPY) {                                                                                   \
+                    _Pragma("unroll") for (int c_ = 0; c_ < W::kCopies / T; ++c_) HBFP_MX4_COPY(W::kCopies / T * i_ + c_, ring); \
+                    if (i_ == T - 1) HBFP_MX4_COPY_LAST(ring);                                                \
+                }                                                                                             \
+            }                                                                                                 \
+            HBFP_MX4_FENCE;                                                                                   \
+        }                                                                                                     \
+        _Pragma("unroll") for (int i_ = 0; i_ < T; ++i_) {                                                    \
+            as[0][i_] = as[1][i_];                                                                            \
+            bs[0][i_] = bs[1][i_];                                                                            \
+        }                                                                                                     \
+        ring = next;                                                                                          \
+    }
+
+    // prologue: up to RING stages on their way, the fragments of k-step 0 when the first has landed
+    HBFP_MX4_COPY_STAGE(0);
+    if (RING > 2 && nstage > 2) {
+        HBFP_MX4_COPY_STAGE(1);
+        HBFP_MX4_COPY_STAGE(2);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (W::kCopies + 1)) : "memory");
+    } else if (nstage > 1) {
+        HBFP_MX4_COPY_STAGE(1);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(W::kCopies + 1) : "memory");
+    } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+        HBFP_MX4_READ(0, lds, 0, i);
+        HBFP_MX4_READ_SCALES(0, lds, i);
+        as[1][i] = bs[1][i] = 0;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (RING > 3 && nstage > 3) HBFP_MX4_COPY_STAGE(3);
+    int ring = 0;
+    int st = 0;
+    for (; st + RING < nstage; ++st) HBFP_MX4_STAGE(RING - 2, true, false);
+    if (RING > 3 && nstage - st == 4) {
+        HBFP_MX4_STAGE(2, false, false);
+        ++st;
+    }
+    if (RING > 2 && nstage - st == 3) {
+        HBFP_MX4_STAGE(1, false, false);
+        ++st;
+    }
+    if (nstage - st == 2) HBFP_MX4_STAGE(0, false, false);
+    HBFP_MX4_STAGE(0, false, true);
+#undef HBFP_MX4_STAGE
+#undef HBFP_MX4_KSTEP
+#undef HBFP_MX4_ROW
+#undef HBFP_MX4_READ_SCALES
+#undef HBFP_MX4_READ
+#undef HBFP_MX4_FENCE
+#undef HBFP_MX4_COPY_STAGE
+#undef HBFP_MX4_COPY_LAST
+#undef HBFP_MX4_COPY
+
+    const int64_t i0 = row0 + 32 * T * wm, j0 = col0 + 32 * T * wn;
+    if (T == 2 && p.splits > 1) {
+        store_result<T, T, false>(p.partial + ((int64_t)split * M + i0) * N + j0, N, M - i0, N - j0, false, lane,
+                                  [&](int i, int j, int v) { return acc[i][j][v]; });
+        return;
+    }
+    float bias[T];
+    const bool has_bias = q.bias != nullptr;
+#pragma unroll
+    for (int j = 0; j < T; ++j) {
+        const int64_t col = j0 + 32 * j + l32;
+        bias[j] = has_bias ? q.bias[col < N ? col : N - 1] : 0.0f;
+    }
+    const auto value = [&](int i, int j, int v) { return has_bias ? acc[i][j][v] + bias[j] : acc[i][j][v]; };
+    if constexpr (OUT == kWideF32) store_result<T, T, STREAM>((float *)q.y + i0 * q.ldy + j0, q.ldy, M - i0, N - j0, false, lane, value);
+    else
+        store_result16<T, T, OUT>((uint16_t *)q.y + i0 * q.ldy + j0, q.ldy, M - i0, N - j0,
+                                  ((uint64_t)(uintptr_t)q.y | (uint64_t)q.ldy * 2) % 4 == 0, lane, value);
+}
+
+// The slices of a product split along k, summed in their order.  A thread sums four outputs 256 apart.
+template <int OUT>
+__global__ __launch_bounds__(256) void mx4_sum_kernel(const Mx4Params p) {
+    const Mx4Product &q = p.q;
+    const int64_t N = q.b.rows, n = q.a.rows * N;
+    const int64_t e0 = (int64_t)blockIdx.x * 1024 + threadIdx.x;
+    float sum[4] = {0, 0, 0, 0};
+    for (int z = 0; z < p.splits; z += 8) {
+        float v[4][8];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[u][k] = e0 + u * 256 < n && z + k < p.splits ? p.partial[(int64_t)(z + k) * n + e0 + u * 256] : 0.0f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[u] += v[u][k];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int64_t e = e0 + u * 256;
+        if (e >= n) return;
+        const int64_t row = n < ((int64_t)1 << 31) ? (int64_t)((uint32_t)e / (uint32_t)N) : e / N, col = e - row * N;
+        store_float<OUT - 1>(q.y, row * q.ldy + col, q.bias ? sum[u] + q.bias[col] : sum[u]);
+    }
+}
+
+// ---- few tokens: one pass over b.  A wave has 16 channels, MT x 16 tokens and a share of the groups; the waves' sums meet in LDS, in
+// the order of the waves.  Lane c + 16 g of a fragment has the blocks 2 g and 2 g + 1 of row c of a group, for two matrix instructions,
+// so that the four lanes of a row read its whole line.  U groups are on their way at once.
+// FUSED: x is converted by every workgroup for itself, into LDS, while the first of b are on their way.
+struct Mx4FewParams {
+    Mx4Product q;
+    const void *x;
+    int64_t ldx;
+    int32_t groups, tiles_n;
+};
+constexpr int kMx4FusedBytes = 32768;       // of codes
+
+template <int MT, int U, int W, int DT, bool FUSED>
+__global__ __launch_bounds__(64 * W) void gemm_mx4_few_kernel(const Mx4FewParams p) {
+    __shared__ v4f sums[W][MT][64];
+    __shared__ __attribute__((aligned(16))) uint8_t own[FUSED ? kMx4FusedBytes : 16];
+    __shared__ __attribute__((aligned(16))) uint8_t own_scales[FUSED ? kMx4FusedBytes / 16 : 16];
+    const Mx4Product &q = p.q;
+    const int t = threadIdx.x, lane = t & 63, c = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int64_t M = q.a.rows, N = q.b.rows;
+    const int64_t n0 = (int64_t)(blockIdx.x % p.tiles_n) * 16, m0 = (int64_t)(blockIdx.x / p.tiles_n) * 16 * MT;
+    const int64_t nr = n0 + c < N ? n0 + c : N - 1;
+    const uint8_t *const b = q.b.codes + nr * 128 + 32 * g, *const bs = q.b.scales + nr * 8 + 2 * g;
+    const int64_t b_step = N * 128, bs_step = q.b.scale_rows * 8, a_step = M * 128, as_step = q.a.scale_rows * 8;
+    const uint8_t *a[MT], *as[MT];
+    if constexpr (!FUSED) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int64_t mr = m0 + 16 * i + c < M ? m0 + 16 * i + c : M - 1;
+            a[i] = q.a.codes + mr * 128 + 32 * g;
+            as[i] = q.a.scales + mr * 8 + 2 * g;
+        }
+    }
+    v4i bw[U][2], aw[U][MT][2];
+    int bsw[U], asw[U][MT];
+    const auto request = [&](int s0) {                      // groups s0, s0 + W, ...; past the end the last one again
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = s0 + u * W < p.groups ? s0 + u * W : p.groups - 1;
+            bw[u][0] = *reinterpret_cast<const v4i *>(b + at * b_step);
+            bw[u][1] = *reinterpret_cast<const v4i *>(b + at * b_step + 16);
+            bsw[u] = *reinterpret_cast<const uint16_t *>(bs + at * bs_step);
+            if constexpr (!FUSED) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    aw[u][i][0] = *reinterpret_cast<const v4i *>(a[i] + at * a_step);
+                    aw[u][i][1] = *reinterpret_cast<const v4i *>(a[i] + at * a_step + 16);
+                    asw[u][i] = *reinterpret_cast<const uint16_t *>(as[i] + at * as_step);
+                }
+            }
+        }
+    };
+    request(wave);
+    const int row_bytes = p.groups * 128;
+    if constexpr (FUSED) {
+        const int64_t K = q.b.kdim;
+        for (int m = 0; m < (int)M; ++m) {
+            for (int64_t k = 8 * t; k < p.groups * 256; k += 512 * W) {
+                float x[8];
+                const int64_t left = K - k;
+                load8<DT>(p.x, m * p.ldx + k, left < 8 ? (int)(left < 0 ? 0 : left) : 8, x);
+                const uint32_t byte = mx4_byte<HBFP_RNE>(largest_of_quad(mx4_largest8(x)));
+                *reinterpret_cast<uint32_t *>(own + m * row_bytes + k / 2) = mx4_codes8(x, byte);
+                if (t % 4 == 0) own_scales[(m * row_bytes + k / 2) / 16] = (uint8_t)byte;
+            }
+        }
+        __syncthreads();
+    }
+    v4f acc[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = wave; s0 < p.groups; s0 += W * U) {
+        if (s0 != wave) request(s0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = s0 + u * W;
+            if (s < p.groups) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    if constexpr (FUSED) {
+                        const int at = (c < M ? c : 0) * row_bytes + s * 128 + 32 * g;
+                        aw[u][i][0] = *reinterpret_cast<const v4i *>(own + at);
+                        aw[u][i][1] = *reinterpret_cast<const v4i *>(own + at + 16);
+                        asw[u][i] = *reinterpret_cast<const uint16_t *>(own_scales + at / 16);
+                    }
+                    acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(four_bit(bw[u][0]), four_bit(aw[u][i][0]), acc[i], 4, 4, 0, bsw[u], 0,
+                                                                              asw[u][i]);
+                    acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(four_bit(bw[u][1]), four_bit(aw[u][i][1]), acc[i], 4, 4, 1, bsw[u], 1,
+                                                                              asw[u][i]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+    // lane: token c, channels 4 g + v; wave w finishes the token tiles w, w + W, ...
+    for (int i = wave; i < MT; i += W) {
+        v4f all = sums[0][i][lane];
+#pragma unroll
+        for (int w = 1; w < W; ++w) all += sums[w][i][lane];
+        const int64_t m = m0 + 16 * i + c;
+        if (m >= M) continue;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int64_t n = n0 + 4 * g + v;
+            if (n < N) store_float<DT>(q.y, m * q.ldy + n, q.bias ? all[v] + q.bias[n] : all[v]);
+        }
+    }
+}
+
+template <int MT, int U, int W, int DT, bool FUSED>
+int launch_few(Mx4FewParams p, hipStream_t s) {
+    p.groups = (int32_t)p.q.b.groups;
+    p.tiles_n = (int32_t)ceil_div(p.q.b.rows, 16);
+    const int64_t wgs = p.tiles_n * ceil_div(p.q.a.rows, 16 * MT);
+    if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
+    hipLaunchKernelGGL((gemm_mx4_few_kernel<MT, U, W, DT, FUSED>), dim3((unsigned)wgs), dim3(64 * W), 0, s, p);
+    return launch_status();
+}
+template <int DT>
+int launch_few_of(const Mx4FewParams &p, hipStream_t s) {
+    if (p.q.a.rows > 16) return launch_few<2, 1, 16, DT, false>(p, s);
+    return launch_few<1, 4, 8, DT, false>(p, s);
+}
+template <int DT>
+int launch_fused_of(const Mx4FewParams &p, hipStream_t s) {
+    return launch_few<1, 2, 16, DT, true>(p, s);
+}
+
+struct Mx4Plan {
+    int T, splits;
+};
+Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t groups) {
+    const int64_t tiles4 = ceil_div(M, 256) * ceil_div(N, 256), tiles2 = ceil_div(M, 128) * ceil_div(N, 128);
+    if (tiles4 >= 192) return {4, 1};
+    int64_t splits = 1;
+    while (tiles2 * splits * 2 <= 512 && groups / (splits * 2) >= 4 && splits < 16) splits *= 2;
+    return {2, (int)splits};
+}
+
+template <int T, int RING, int OUT>
+int launch_tiles(const Mx4Params &p, bool stream, hipStream_t s) {
+    static std::atomic<bool> configured[2];
+    constexpr int lds_bytes = Mx4Tile<T, RING>::kLds;
+    constexpr bool kStreams = OUT == kWideF32;      // (16-bit outputs leave by ordinary stores)
+    stream = stream && kStreams;
+    void (*const kernel)(Mx4Params) = stream ? &gemm_mx4_kernel<T, RING, OUT, kStreams> : &gemm_mx4_kernel<T, RING, OUT, false>;
+    if (allow_dynamic_lds(configured[stream], reinterpret_cast<const void *>(kernel), lds_bytes) != HBFP_OK) return HBFP_ERR_LAUNCH;
+    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+    const dim3 grid = p.splits >= 8 ? dim3((unsigned)(8 * tiles * ceil_div(p.splits, 8))) : dim3((unsigned)(ceil_div(tiles, 8) * 8), (unsigned)p.splits);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), lds_bytes, s, p);
+    return launch_status();
+}
+template <int OUT>
+int launch_planned(Mx4Params p, const Mx4Plan &plan, hipStream_t s) {
+    p.groups = (int32_t)p.q.b.groups;
+    p.groups_per_split = (int32_t)ceil_div(p.groups, plan.splits);
+    p.splits = (int32_t)ceil_div(p.groups, p.groups_per_split);
+    p.tiles_m = (int32_t)ceil_div(p.q.a.rows, 64 * plan.T);
+    p.tiles_n = (int32_t)ceil_div(p.q.b.rows, 64 * plan.T);
+    GemmArgs g = {};
+    g.M = p.q.a.rows;
+    g.N = p.q.b.rows;
+    g.C = (float *)p.q.y;
+    g.ldc = p.q.ldy;
+    const bool stream = stores_stream(&g);
+    const int rc = plan.T == 4 ? launch_tiles<4, 2, OUT>(p, stream, s) : launch_tiles<2, 2, OUT>(p, stream, s);
+    if (rc != HBFP_OK || p.splits == 1) return rc;
+    const int64_t wgs = ceil_div(g.M * g.N, 1024);
+    if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
+    hipLaunchKernelGGL(mx4_sum_kernel<OUT>, dim3((unsigned)wgs), dim3(256), 0, s, p);
+    return launch_status();
+}
+
+bool few_rows(int64_t M, int64_t, int64_t) { return M <= 16; }
+
+}  // namespace
+
+size_t gemm_mx4_workspace(int64_t M, int64_t N, int64_t groups) {
+    if (few_rows(M, N, groups)) return 0;
+    const Mx4Plan plan = mx4_plan(M, N, groups);
+    return plan.splits > 1 ? (size_t)plan.splits * (size_t)M * (size_t)N * 4 : 0;
+}
+
+int launch_gemm_mx4(const Mx4Product &q, void *workspace, hipStream_t s) {
+    const int64_t M = q.a.rows, N = q.b.rows, groups = q.b.groups;
+    if (few_rows(M, N, groups)) {
+        const Mx4FewParams p = {q, nullptr, 0, 0, 0};
+        return q.dtype == HBFP_F32 ? launch_few_of<HBFP_F32>(p, s) : q.dtype == HBFP_BF16 ? launch_few_of<HBFP_BF16>(p, s) : launch_few_of<HBFP_F16>(p, s);
+    }
+    if (ceil_div(M, 128) * ceil_div(N, 128) > 0x7ffffff0) return HBFP_ERR_ARG;
+    const Mx4Plan plan = mx4_plan(M, N, groups);
+    const Mx4Params p = {q, (float *)workspace, 0, 0, 0, 0, 0};
+    return q.dtype == HBFP_F32    ? launch_planned<kWideF32>(p, plan, s)
+           : q.dtype == HBFP_BF16 ? launch_planned<kWideBf16>(p, plan, s)
+                                  : launch_planned<kWideF16>(p, plan, s);
+}
+
+bool linear_mx4_fused_ok(int64_t M, int64_t, int64_t groups) { return M <= 2 && M * groups * 128 <= kMx4FusedBytes; }
+
+int launch_linear_mx4_fused(const Mx4Product &q, const void *x, int64_t ldx, hipStream_t s) {
+    const Mx4FewParams p = {q, x, ldx, 0, 0};
+    return q.dtype == HBFP_F32 ? launch_fused_of<HBFP_F32>(p, s) : q.dtype == HBFP_BF16 ? launch_fused_of<HBFP_BF16>(p, s) : launch_fused_of<HBFP_F16>(p, s);
+}
+
+}  // namespace hbfp

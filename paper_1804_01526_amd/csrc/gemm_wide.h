@@ -400,7 +400,7 @@ int launch_wide_t(WideParams p, bool stream, hipStream_t s) {
 struct WidePlan {
     int T, splits;
 };
-WidePlan wide_plan(int64_t M, int64_t N, int64_t nstage, bool may_split) {
+[[maybe_unused]] WidePlan wide_plan(int64_t M, int64_t N, int64_t nstage, bool may_split) {
     static const double base[3] = {3.1, 1.6, 5.1}, lone[3] = {0.17, 0.30, 0.48}, full[3] = {0.32, 0.50, 0.86}, tail[3] = {3.0, 8.4, 10.9};
     WidePlan best = {2, 1};
     double least = 0.0;

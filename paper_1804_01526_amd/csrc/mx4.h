@@ -1,0 +1,107 @@
+// Microscaled 4-bit operands (layout and arithmetic in the public header): launchers, and the device side of the conversion.
+#pragma once
+#include "bfp_device.h"
+#include "kv_cache.h"
+
+namespace hbfp {
+
+struct Mx4View {
+    uint8_t *codes, *scales;
+    int64_t rows, kdim, groups, scale_rows;
+};
+
+// mx4_quant.hip
+int launch_quant_mx4(const void *src, int dtype, int64_t rows, int64_t cols, int64_t ld, int rounding, uint64_t seed, const Mx4View *along,
+                     const Mx4View *down, hipStream_t s);
+int launch_read_mx4(const Mx4View &t, int dtype, void *dst, int64_t ld, hipStream_t s);
+
+// gemm_mx4.hip
+struct Mx4Product {
+    Mx4View a, b;
+    const float *bias;
+    void *y;
+    int64_t ldy;
+    int32_t dtype;
+};
+size_t gemm_mx4_workspace(int64_t M, int64_t N, int64_t groups);
+int launch_gemm_mx4(const Mx4Product &p, void *workspace, hipStream_t s);
+// x converted inside the product: few tokens whose codes fit into LDS; p.a's buffers are not read
+bool linear_mx4_fused_ok(int64_t M, int64_t N, int64_t groups);
+int launch_linear_mx4_fused(const Mx4Product &p, const void *x, int64_t ldx, hipStream_t s);
+
+// norm.hip
+struct NormArgs {
+    hbfp_norm n;
+    int8_t *codes;               // int8 rows of kpad bytes and a scale each, or
+    float *scales;
+    int64_t kpad;
+    Mx4View mx4;                 // (codes NULL)
+};
+int launch_norm(const NormArgs &a, hipStream_t s);
+struct NormGradArgs {
+    const void *g, *sum, *g_sum;
+    const float *rstd, *weight;
+    void *dx;
+    float *dweight, *partial;
+    int64_t ldg, ld_sum, ld_g_sum, ldx, rows, cols;
+    int32_t dtype;
+};
+size_t norm_grad_workspace(int64_t rows, int64_t cols);
+int launch_norm_grad(const NormGradArgs &a, hipStream_t s);
+
+namespace {
+
+// the byte of a block from the bit pattern of its largest magnitude: adding what rounds up carries into the exponent field
+template <int ROUND>
+__device__ __forceinline__ uint32_t mx4_byte(uint32_t amax) {
+    if (amax >= 0x7f800000u) return 255u;
+    uint32_t e = (amax + (ROUND == HBFP_RNE ? 0x200000u : 0x3fffffu)) >> 23;
+    e = e > 254u ? 254u : e;
+    return e < 2u ? 0u : e - 2u;
+}
+
+// eight values -> a word of codes, to nearest.  The instruction divides by a power of two of which it reads the exponent field alone
+// (0: 2^-127), rounds to nearest even and cuts at 6; the builtin writes one byte of the word.
+__device__ __forceinline__ uint32_t mx4_codes8(const float *x, uint32_t byte) {
+    const float unit = __uint_as_float(byte << 23);
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], unit, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], unit, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], unit, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], unit, 3);
+    return byte == 255u ? 0u : w;
+}
+
+// ... stochastically.  |x| in units is exact in FP32 (but for values that vanish); a step is 1/2, 1 or 2 units, and q steps are the code q,
+// q + 2 and q + 4.  The fraction of a step times 2^32, cut to an integer, decides as the exact one does: h is an integer.
+__device__ __forceinline__ uint32_t mx4_code_sr(float x, int neg_exp, uint32_t h) {
+    const float a = __builtin_amdgcn_ldexpf(__builtin_fabsf(x), neg_exp);
+    const int up = a < 2.0f ? 0 : a < 4.0f ? 1 : 2;
+    const float t = __builtin_amdgcn_ldexpf(a, 1 - up);
+    const uint32_t whole = (uint32_t)t;
+    const uint32_t frac = (uint32_t)__builtin_amdgcn_ldexpf(__builtin_amdgcn_fractf(t), 32);
+    uint32_t code = whole + ((frac + h) < h ? 1u : 0u) + 2u * (uint32_t)up;
+    code = code > 7u ? 7u : code;
+    return code | (__float_as_uint(x) >> 31) << 3;
+}
+
+// largest magnitude of eight values, as bits (a NaN is larger than everything)
+__device__ __forceinline__ uint32_t mx4_largest8(const float *x) {
+    uint32_t amax = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t a = __float_as_uint(x[i]) & 0x7fffffffu;
+        amax = a > amax ? a : amax;
+    }
+    return amax;
+}
+// ... of four neighbouring lanes: a block of 32
+__device__ __forceinline__ uint32_t largest_of_quad(uint32_t a) {
+    uint32_t b = (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0xB1, 0xF, 0xF, true);      // lanes 1, 0, 3, 2
+    a = b > a ? b : a;
+    b = (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0x4E, 0xF, 0xF, true);               // lanes 2, 3, 0, 1
+    return b > a ? b : a;
+}
+
+}  // namespace
+}  // namespace hbfp

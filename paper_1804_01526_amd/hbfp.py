@@ -77,6 +77,20 @@ class Heads(ctypes.Structure):
                 ("stride_batch", ctypes.c_int64), ("stride_token", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
 
 
+class Mx4Desc(ctypes.Structure):
+    """hbfp_mx4: an operand in microscaled 4-bit floating point (layout in include/hbfp.h)."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64), ("kdim", ctypes.c_int64),
+                ("groups", ctypes.c_int64), ("scale_rows", ctypes.c_int64), ("code_bytes", ctypes.c_uint64), ("scale_bytes", ctypes.c_uint64)]
+
+
+class NormDesc(ctypes.Structure):
+    """hbfp_norm: the arguments of a norm that do not depend on the form of its result."""
+    _fields_ = [("x", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("sum", ctypes.c_void_p),
+                ("values", ctypes.c_void_p), ("rstd", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ldx", ctypes.c_int64), ("ld_residual", ctypes.c_int64), ("ld_sum", ctypes.c_int64), ("ld_values", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
 def _load():
     if not os.path.exists(_LIB_PATH):
         raise ImportError(
@@ -157,6 +171,21 @@ def _load():
     lib.hbfp_gemm_rows.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, i32, i64, vp, sz, vp]
     lib.hbfp_linear_i8_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(sz)]
     lib.hbfp_linear_i8.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, i64, vp, i64, vp, sz, vp]
+    X, size = ctypes.POINTER(Mx4Desc), ctypes.POINTER(sz)
+    lib.hbfp_mx4_plan.argtypes = [i64, i64, X]
+    lib.hbfp_quant_mx4.argtypes = [vp, i32, i64, i64, i64, i32, ctypes.c_uint64, X, X, vp]
+    lib.hbfp_read_mx4.argtypes = [X, i32, vp, i64, vp]
+    lib.hbfp_gemm_mx4_workspace.argtypes = [i64, i64, i64, size]
+    lib.hbfp_gemm_mx4.argtypes = [X, X, vp, vp, i32, i64, vp, sz, vp]
+    lib.hbfp_linear_mx4_workspace.argtypes = [i64, i64, i64, size]
+    lib.hbfp_linear_mx4.argtypes = [vp, i32, i64, i64, X, vp, vp, i64, vp, sz, vp]
+    lib.hbfp_norm_i8.argtypes = [ctypes.POINTER(NormDesc), vp, vp, vp]
+    lib.hbfp_norm_mx4.argtypes = [ctypes.POINTER(NormDesc), X, vp]
+    lib.hbfp_norm_grad_workspace.argtypes = [i64, i64, size]
+    lib.hbfp_norm_grad.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, i32, i64, i64, vp, i64, vp, vp, sz, vp]
+    for name in ("hbfp_mx4_plan", "hbfp_quant_mx4", "hbfp_read_mx4", "hbfp_gemm_mx4_workspace", "hbfp_gemm_mx4", "hbfp_linear_mx4_workspace",
+                 "hbfp_linear_mx4", "hbfp_norm_i8", "hbfp_norm_mx4", "hbfp_norm_grad_workspace", "hbfp_norm_grad"):
+        getattr(lib, name).restype = i32
     for name in ("hbfp_cache_plan", "hbfp_cache_append", "hbfp_cache_read", "hbfp_cache_attend_workspace", "hbfp_cache_attend",
                  "hbfp_cache_weigh", "hbfp_cache_weigh_longest", "hbfp_cache_evict", "hbfp_rows_plan", "hbfp_quant_rows", "hbfp_gemm_rows_workspace",
                  "hbfp_gemm_rows", "hbfp_linear_i8_workspace", "hbfp_linear_i8"):
@@ -691,10 +720,20 @@ def _there(stream, device, call, *args):
     caller = torch.cuda.current_stream(device)
     with torch.cuda.device(device) if stream is None else torch.cuda.stream(stream):
         result = call(*args)
-    for t in (result.codes, result.scales) if isinstance(result, RowCodes) else result if isinstance(result, tuple) else (result,):
-        if stream is not None and t is not None and t.numel():
-            t.record_stream(caller)
+    if stream is not None:
+        for t in _buffers(result):
+            if t.numel():
+                t.record_stream(caller)
     return result
+
+
+def _buffers(result):
+    """The tensors that a call returns."""
+    if isinstance(result, (RowCodes, Mx4)):
+        return [result.codes, result.scales]
+    if isinstance(result, tuple):
+        return [t for r in result for t in _buffers(r)]
+    return [] if result is None else [result]
 
 
 def _heads(t: torch.Tensor, batch: int, tokens: int, heads: int, dim: int, device) -> Heads:
@@ -946,3 +985,199 @@ def linear_i8(x: torch.Tensor, w: RowCodes, bias: Optional[torch.Tensor] = None,
                                _ptr(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(x.device)),
            "hbfp_linear_i8")
     return out
+
+
+# ---------------------------------------------------------------------------- microscaled 4-bit floating point
+@dataclass
+class Mx4:
+    """An operand of products in microscaled 4-bit floating point: the descriptor plus the torch buffers behind its two pointers."""
+    desc: Mx4Desc
+    codes: torch.Tensor    # uint8 [groups, rows, 128]
+    scales: torch.Tensor   # uint8 [groups, rows rounded up to 16, 8]
+
+
+def mx4_plan(rows: int, kdim: int) -> Mx4Desc:
+    d = Mx4Desc()
+    _check(_lib.hbfp_mx4_plan(rows, kdim, ctypes.byref(d)), "hbfp_mx4_plan")
+    return d
+
+
+def mx4_alloc(rows: int, kdim: int, device="cuda") -> Mx4:
+    """An operand of `rows` rows and a contraction of `kdim` (its contents are whatever the memory holds)."""
+    d = mx4_plan(rows, kdim)
+    codes = torch.empty((d.groups, rows, 128), dtype=torch.uint8, device=device)
+    scales = torch.empty((d.groups, d.scale_rows, 8), dtype=torch.uint8, device=device)
+    d.codes, d.scales = codes.data_ptr(), scales.data_ptr()
+    return Mx4(d, codes, scales)
+
+
+def _quant_mx4(x, along, down, rounding, seed):
+    rows, cols = x.shape
+    a = mx4_alloc(rows, cols, x.device) if along else None
+    d = mx4_alloc(cols, rows, x.device) if down else None
+    _check(_lib.hbfp_quant_mx4(_ptr(x), _TYPES[x.dtype], rows, cols, _matrix(x), rounding, seed, ctypes.byref(a.desc) if a else None,
+                               ctypes.byref(d.desc) if d else None, _raw_stream(x.device)), "hbfp_quant_mx4")
+    return a, d
+
+
+def quant_mx4(x: torch.Tensor, axis: int = 1, rounding: int = RNE, seed: int = 0, stream=None) -> Mx4:
+    """hbfp_quant_mx4 of x [rows, cols] with the contraction along its rows (axis 1: weights [out features, in features], tokens) or down
+    its columns (axis 0: the operand's rows are x's columns)."""
+    _matrix(x)
+    assert axis in (0, 1)
+    if stream is not None or _current_device() != x.device.index:
+        return _there(stream, x.device, quant_mx4, x, axis, rounding, seed)
+    return _quant_mx4(x, axis == 1, axis == 0, rounding, seed)[1 - axis]
+
+
+def quant_mx4_both(x: torch.Tensor, rounding: int = RNE, seed: int = 0, stream=None):
+    """hbfp_quant_mx4 of x into both operands, (along its rows, down its columns), from one read: what a training step needs of a matrix."""
+    _matrix(x)
+    if stream is not None or _current_device() != x.device.index:
+        return _there(stream, x.device, quant_mx4_both, x, rounding, seed)
+    return _quant_mx4(x, True, True, rounding, seed)
+
+
+def read_mx4(t: Mx4, dtype=torch.float32, stream=None) -> torch.Tensor:
+    """hbfp_read_mx4: the values [rows, kdim] that an operand holds, in FP32 or bf16."""
+    device = t.codes.device
+    if stream is not None or _current_device() != device.index:
+        return _there(stream, device, read_mx4, t, dtype)
+    out = torch.empty((t.desc.rows, t.desc.kdim), dtype=dtype, device=device)
+    _check(_lib.hbfp_read_mx4(ctypes.byref(t.desc), _TYPES[dtype], _ptr(out), t.desc.kdim, _raw_stream(device)), "hbfp_read_mx4")
+    return out
+
+
+@functools.lru_cache(maxsize=1024)
+def gemm_mx4_workspace(rows: int, out_features: int, in_features: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.hbfp_gemm_mx4_workspace(rows, out_features, in_features, ctypes.byref(n)), "hbfp_gemm_mx4_workspace")
+    return int(n.value)
+
+
+@functools.lru_cache(maxsize=1024)
+def linear_mx4_workspace(rows: int, out_features: int, in_features: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.hbfp_linear_mx4_workspace(rows, out_features, in_features, ctypes.byref(n)), "hbfp_linear_mx4_workspace")
+    return int(n.value)
+
+
+def _mx4_out(bias, w: Mx4, rows: int, dtype, device, out):
+    n = w.desc.rows
+    assert w.codes.device == device
+    if bias is not None:
+        assert bias.device == device and bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == n
+    if out is None:
+        out = torch.empty((rows, n), dtype=dtype, device=device)
+    assert out.device == device and out.dtype == dtype and tuple(out.shape) == (rows, n)
+    return out, _matrix(out)
+
+
+def gemm_mx4(a: Mx4, b: Mx4, bias: Optional[torch.Tensor] = None, dtype=torch.float32, out: Optional[torch.Tensor] = None,
+             workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """hbfp_gemm_mx4: y [rows of a, rows of b] = a . b^T (+ bias), rounded once to `dtype`."""
+    m, n, device = a.desc.rows, b.desc.rows, a.codes.device
+    if stream is not None or _current_device() != device.index:
+        return _there(stream, device, gemm_mx4, a, b, bias, dtype, out, workspace)
+    out, ld = _mx4_out(bias, b, m, dtype if out is None else out.dtype, device, out)
+    if workspace is None:
+        workspace = _workspace(gemm_mx4_workspace(m, n, a.desc.kdim), device)
+    _check(_lib.hbfp_gemm_mx4(ctypes.byref(a.desc), ctypes.byref(b.desc), _ptr(bias), _ptr(out), _TYPES[out.dtype], ld, _ptr(workspace),
+                              0 if workspace is None else workspace.numel(), _raw_stream(device)), "hbfp_gemm_mx4")
+    return out
+
+
+def linear_mx4(x: torch.Tensor, w: Mx4, bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """hbfp_linear_mx4: y = quant(x) . w^T (+ bias) in x's type, for x [tokens, in features] and weights from quant_mx4."""
+    ldx, (m, k), n = _matrix(x), x.shape, w.desc.rows
+    if stream is not None or _current_device() != x.device.index:
+        return _there(stream, x.device, linear_mx4, x, w, bias, out, workspace)
+    assert k == w.desc.kdim
+    out, ldy = _mx4_out(bias, w, m, x.dtype, x.device, out)
+    if workspace is None:
+        workspace = _workspace(linear_mx4_workspace(m, n, k), x.device)
+    _check(_lib.hbfp_linear_mx4(_ptr(x), _TYPES[x.dtype], m, ldx, ctypes.byref(w.desc), _ptr(bias), _ptr(out), ldy, _ptr(workspace),
+                                0 if workspace is None else workspace.numel(), _raw_stream(x.device)), "hbfp_linear_mx4")
+    return out
+
+
+# ---------------------------------------------------------------------------- the norm in front of a quantised product
+def _like(t: Optional[torch.Tensor], x: torch.Tensor) -> int:
+    """The leading dimension of a matrix that goes with x; 0 for none."""
+    if t is None:
+        return 0
+    assert t.device == x.device and t.dtype == x.dtype and t.shape == x.shape, "a matrix of x's shape and type on its GPU"
+    return _matrix(t)
+
+
+def _vector(t: Optional[torch.Tensor], n: int, device):
+    if t is not None:
+        assert t.device == device and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n, "a contiguous FP32 vector"
+    return _ptr(t)
+
+
+def _norm(x, weight, eps, residual, total, values):
+    """The arguments of a norm, and what it returns beside its codes."""
+    ldx, (rows, cols), device = _matrix(x), x.shape, x.device
+    if total is None:
+        total = torch.empty((rows, cols), dtype=x.dtype, device=device) if residual is not None else x
+    held = torch.empty((rows, cols), dtype=x.dtype, device=device) if values else None
+    rstd = torch.empty((rows,), dtype=torch.float32, device=device)
+    stored = None if total is x and residual is None else total
+    desc = NormDesc(_ptr(x), _ptr(residual), _vector(weight, cols, device), _ptr(stored), _ptr(held), _ptr(rstd), rows, cols, ldx,
+                    _like(residual, x), _like(stored, x), cols, _TYPES[x.dtype], eps)
+    return desc, total, rstd, held
+
+
+def norm_i8(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float = 1e-6, residual: Optional[torch.Tensor] = None,
+            out_sum: Optional[torch.Tensor] = None, values: bool = False, stream=None):
+    """hbfp_norm_i8 of x + residual: (rows for gemm_rows, the sum, 1 / rms of each row, the codes' values in x's type or None).  weight:
+    FP32 [cols] or None.  out_sum: where the sum goes (x and residual are allowed); without a residual the sum is x itself."""
+    _matrix(x)
+    if stream is not None or _current_device() != x.device.index:
+        return _there(stream, x.device, norm_i8, x, weight, eps, residual, out_sum, values)
+    desc, total, rstd, held = _norm(x, weight, eps, residual, out_sum, values)
+    kpad = ctypes.c_int64(0)
+    _check(_lib.hbfp_rows_plan(x.shape[0], x.shape[1], ctypes.byref(kpad), None), "hbfp_rows_plan")
+    codes = torch.empty((x.shape[0], kpad.value), dtype=torch.int8, device=x.device)
+    scales = torch.empty((x.shape[0],), dtype=torch.float32, device=x.device)
+    _check(_lib.hbfp_norm_i8(ctypes.byref(desc), _ptr(codes), _ptr(scales), _raw_stream(x.device)), "hbfp_norm_i8")
+    return RowCodes(codes, scales, x.shape[1]), total, rstd, held
+
+
+def norm_mx4(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float = 1e-6, residual: Optional[torch.Tensor] = None,
+             out_sum: Optional[torch.Tensor] = None, values: bool = False, stream=None):
+    """hbfp_norm_mx4: norm_i8 with an operand for gemm_mx4 in the place of the rows."""
+    _matrix(x)
+    if stream is not None or _current_device() != x.device.index:
+        return _there(stream, x.device, norm_mx4, x, weight, eps, residual, out_sum, values)
+    desc, total, rstd, held = _norm(x, weight, eps, residual, out_sum, values)
+    out = mx4_alloc(x.shape[0], x.shape[1], x.device)
+    _check(_lib.hbfp_norm_mx4(ctypes.byref(desc), ctypes.byref(out.desc), _raw_stream(x.device)), "hbfp_norm_mx4")
+    return out, total, rstd, held
+
+
+@functools.lru_cache(maxsize=1024)
+def norm_grad_workspace(rows: int, cols: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.hbfp_norm_grad_workspace(rows, cols, ctypes.byref(n)), "hbfp_norm_grad_workspace")
+    return int(n.value)
+
+
+def norm_grad(g: torch.Tensor, total: torch.Tensor, rstd: torch.Tensor, weight: Optional[torch.Tensor], g_sum: Optional[torch.Tensor] = None,
+              out: Optional[torch.Tensor] = None, weight_grad: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
+    """hbfp_norm_grad: (gradient of x and of the residual, gradient of the weight FP32 [cols] or None) from g, the gradient of the
+    normalised rows, with the sum and rstd that the norm returned; g_sum: what reaches the sum by other ways.  out may be g or g_sum."""
+    ldg, (rows, cols), device = _matrix(g), g.shape, g.device
+    if stream is not None or _current_device() != device.index:
+        return _there(stream, device, norm_grad, g, total, rstd, weight, g_sum, out, weight_grad, workspace)
+    if out is None:
+        out = torch.empty((rows, cols), dtype=g.dtype, device=device)
+    dweight = torch.empty((cols,), dtype=torch.float32, device=device) if weight_grad else None
+    if workspace is None and weight_grad:
+        workspace = _workspace(norm_grad_workspace(rows, cols), device)
+    _check(_lib.hbfp_norm_grad(_ptr(g), ldg, _ptr(total), _like(total, g), _vector(rstd, rows, device), _vector(weight, cols, device),
+                               _ptr(g_sum), _like(g_sum, g), _TYPES[g.dtype], rows, cols, _ptr(out), _like(out, g), _ptr(dweight),
+                               _ptr(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(device)), "hbfp_norm_grad")
+    return out, dweight

@@ -1,0 +1,255 @@
+"""Microscaled 4-bit operands on the GPU against their definitions in 64 bits (tests/mx4_ref.py).
+
+Tolerances.  Codes and scales are exact.  Products: every product of two values is exact in FP64 and, within its block's exponents, in the
+matrix instruction; sums are FP32, one rounding (at most a whole step, 2^-23 relative) for every 64 products and every slice or wave
+that is joined.  With S = sum |a b| an output may be off by
+    u |y|  +  (K / 64 + 80) 2^-23 (S + |bias|)  +  K 2^-126,
+u the unit roundoff of its type (2^-8 bf16, 2^-11 FP16, 2^-24 FP32), the last term for products below FP32's normal range."""
+import numpy as np
+import pytest
+import torch
+
+from tests import mx4_ref
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+U = {F32: 2.0 ** -24, BF16: 2.0 ** -8, F16: 2.0 ** -11}
+
+
+@pytest.fixture(scope="module")
+def hb():
+    from paper_1804_01526_amd import hbfp
+    assert torch.cuda.is_available(), "these tests need the GPU"
+    return hbfp
+
+
+def _np(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def _rand(rng, rows, cols, dtype, spread=3, ld=None):
+    """Rows of a wider buffer whose other columns hold NaN."""
+    x = rng.standard_normal((rows, cols)) * np.exp2(rng.integers(-spread, spread + 1, size=(rows, cols)))
+    wide = torch.full((rows, ld or cols), float("nan"), dtype=dtype, device="cuda")
+    wide[:, :cols] = torch.from_numpy(x.astype(np.float32)).cuda().to(dtype)
+    return wide[:, :cols]
+
+
+def _stored(t):
+    """(codes, scales) of an operand in the layout of the reference; what lies past kdim has to be 0."""
+    d = t.desc
+    raw = t.codes.cpu().numpy()                                              # [groups][rows][128]
+    nib = np.stack([raw & 15, raw >> 4], axis=-1).reshape(d.groups, d.rows, 256)
+    codes = nib.transpose(1, 0, 2).reshape(d.rows, -1).astype(np.int64)
+    scales = t.scales.cpu().numpy()[:, :d.rows].transpose(1, 0, 2).reshape(d.rows, -1).astype(np.int64)
+    nblk = -(-d.kdim // 32)
+    assert not codes[:, d.kdim:].any() and not scales[:, nblk:].any()
+    return codes[:, :d.kdim], scales[:, :nblk]
+
+
+def _same_codes(got, want):
+    """Equal, but for the sign of a zero."""
+    sign = np.where(want & 7, 15, 7)
+    np.testing.assert_array_equal(got & sign, want & sign)
+
+
+# ------------------------------------------------------------------------------------------------------------- conversion
+@pytest.mark.parametrize("rows,cols,ld", [(1, 1, None), (1, 32, None), (5, 33, 40), (33, 256, None), (40, 257, 300), (130, 700, 701), (257, 129, None),
+                                          (300, 31, 33), (1, 5000, None), (2000, 3, 4)])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rounding", [0, 1])
+def test_quant_holds_the_definition_s_codes(hb, rows, cols, ld, dtype, rounding):
+    print(f"[quant] {rows}x{cols} ld {ld} {dtype} rounding {rounding}", flush=True)
+    rng = np.random.default_rng(rows * 7 + cols)
+    x = _rand(rng, rows, cols, dtype, ld=ld)
+    seed = 0x1234567890ABCDEF
+    h = mx4_ref.words(rows, cols, seed) if rounding else None
+    along, down = hb.quant_mx4_both(x, rounding, seed)
+    for got in (along, hb.quant_mx4(x, 1, rounding, seed)):
+        codes, scales = mx4_ref.quant(_np(x), h)
+        np.testing.assert_array_equal(_stored(got)[1], scales)
+        _same_codes(_stored(got)[0], codes)
+    for got in (down, hb.quant_mx4(x, 0, rounding, seed)):
+        codes, scales = mx4_ref.quant(_np(x).T, None if h is None else h.T)
+        np.testing.assert_array_equal(_stored(got)[1], scales)
+        _same_codes(_stored(got)[0], codes)
+    for t, n in ((along, _np(x)), (down, _np(x).T)):
+        want = mx4_ref.held(n, None if h is None else h if t is along else h.T)
+        for out_type in (F32, BF16):
+            np.testing.assert_array_equal(_np(hb.read_mx4(t, out_type)), want)
+
+
+def test_quant_at_the_ends(hb):
+    """Ties, raised exponents, zeros, the smallest and the largest numbers, and blocks that hold an Inf or a NaN."""
+    blocks = [[6, 5, 5.5, 3.5, 2.5, 1.75, 1.25, 0.75, 0.25, 0.2500001, -0.25, -0.75, -5], [7, 5, 1], [6.9999995, 1], [1.75, 1], [1.7499999, 1],
+              [0.0, -0.0], [2.0 ** -127 * 3, 2.0 ** -128, 2.0 ** -129, -2.0 ** -130], [2.0 ** -149], [2.0 ** -126 * 1.75, 2.0 ** -127], [2.0 ** -125, 2.0 ** -128],
+              [3.4e38, -3e38, 1.7e38, 1], [2.0 ** 127 * 1.75, 2.0 ** 126], [float("inf"), 1], [float("nan"), -1], [1, float("-inf"), 2]]
+    x = np.zeros((len(blocks), 64), dtype=np.float32)
+    for i, b in enumerate(blocks):
+        x[i, :len(b)] = b
+        x[i, 32:32 + len(b)] = -np.array(b, dtype=np.float32)
+    dev = torch.from_numpy(x).cuda()
+    for rounding in (0, 1):
+        h = mx4_ref.words(*x.shape, 7) if rounding else None
+        with np.errstate(invalid="ignore"):
+            codes, scales = mx4_ref.quant(x.astype(np.float64), h)
+        got = hb.quant_mx4(dev, 1, rounding, 7)
+        np.testing.assert_array_equal(_stored(got)[1], scales)
+        _same_codes(_stored(got)[0], codes)
+        np.testing.assert_array_equal(np.isnan(_np(hb.read_mx4(got))), np.repeat(scales == 255, 32, axis=1))
+        with np.errstate(invalid="ignore"):
+            codes, scales = mx4_ref.quant(x.T.astype(np.float64), None if h is None else h.T)
+        got = hb.quant_mx4(dev, 0, rounding, 7)
+        np.testing.assert_array_equal(_stored(got)[1], scales)
+        _same_codes(_stored(got)[0], codes)
+
+
+def test_stochastic_rounding_keeps_the_mean(hb):
+    """Of 2^16 roundings of the same number, the mean: a step is at most 2 units, so the mean of n has a standard deviation below
+    1 / sqrt(n) units; six of those are allowed."""
+    row = torch.tensor([6.0, 0.1, 0.4, 1.3, 2.2, 3.9, 4.1, 5.9] + [0.0] * 24, device="cuda")
+    n = 1 << 16
+    got = _np(hb.read_mx4(hb.quant_mx4(row.repeat(n, 1), 1, hb.STOCHASTIC, 99)))
+    assert np.abs(got.mean(axis=0) - _np(row)).max() < 6 / np.sqrt(n)
+
+
+# --------------------------------------------------------------------------------------------------------------- products
+def _check_product(got, a, b, bias, dtype):
+    want, size = a @ b.T, np.abs(a) @ np.abs(b).T
+    if bias is not None:
+        want, size = want + bias, size + np.abs(bias)
+    k = a.shape[1]
+    tol = U[dtype] * np.abs(want) + (k / 64 + 80) * 2.0 ** -23 * size + k * 2.0 ** -126
+    err = np.abs(_np(got) - want)
+    assert (err <= tol).all(), f"{(err / tol).max():.3f} of the tolerance at {np.unravel_index((err / tol).argmax(), err.shape)}"
+
+
+PRODUCTS = [(1, 1, 1), (1, 17, 31), (2, 40, 600), (3, 100, 257), (16, 33, 4100), (16, 4096, 300), (17, 20, 256), (31, 130, 3000), (33, 129, 1000),
+            (64, 128, 256), (128, 128, 2048), (100, 200, 8200), (129, 257, 511), (300, 70, 9000), (500, 1100, 730), (1030, 520, 260),
+            (3500, 3700, 300), (3585, 3580, 800)]
+
+
+@pytest.mark.parametrize("m,n,k", PRODUCTS)
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_gemm(hb, m, n, k, dtype):
+    print(f"[gemm] {m}x{n}x{k} {dtype}", flush=True)
+    rng = np.random.default_rng(m + n + k)
+    a, b = _rand(rng, m, k, F32), _rand(rng, n, k, F32)
+    a *= 2.0 ** -4
+    bias = torch.from_numpy(rng.standard_normal(n).astype(np.float32)).cuda() if (m + n) % 2 else None
+    qa, qb = hb.quant_mx4(a), hb.quant_mx4(b)
+    wide = torch.full((m, n + 3), 77.0, dtype=dtype, device="cuda")
+    got = hb.gemm_mx4(qa, qb, bias, out=wide[:, :n])
+    _check_product(got, mx4_ref.held(_np(a)), mx4_ref.held(_np(b)), None if bias is None else _np(bias), dtype)
+    assert (wide[:, n:] == 77).all()
+    again = hb.gemm_mx4(qa, qb, bias, dtype=dtype)
+    assert torch.equal(again, got)                                                  # the same bits, wherever y lies
+
+
+@pytest.mark.parametrize("m,n,k,bias", [(1, 1, 1, False), (1, 100, 5000, True), (2, 4096, 4096, False), (1, 4096, 65536, False), (1, 50, 65537, True),
+                                        (3, 40, 300, True), (16, 1000, 513, False), (40, 300, 700, True), (260, 300, 1000, False)])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_linear(hb, m, n, k, bias, dtype):
+    print(f"[linear] {m}x{n}x{k} {dtype}", flush=True)
+    rng = np.random.default_rng(m + n + k)
+    x, w = _rand(rng, m, k, dtype, spread=1, ld=k + 5), _rand(rng, n, k, BF16, spread=1)
+    x *= 2.0 ** -3
+    b = torch.from_numpy(rng.standard_normal(n).astype(np.float32)).cuda() if bias else None
+    qw = hb.quant_mx4(w)
+    got = hb.linear_mx4(x, qw, b)
+    assert got.dtype == dtype
+    _check_product(got, mx4_ref.held(_np(x)), mx4_ref.held(_np(w)), None if b is None else _np(b), dtype)
+
+
+def test_products_of_far_exponents(hb):
+    """Blocks whose scales differ by up to 2^100, the smallest and the largest results."""
+    rng = np.random.default_rng(3)
+    for m in (5, 40):
+        x, w = (np.asarray(rng.standard_normal((r, 700)) * np.exp2(rng.integers(-50, 51, size=(r, 22)).repeat(32, axis=1)[:, :700]), np.float32) for r in (m, 50))
+        qa, qw = hb.quant_mx4(torch.from_numpy(x).cuda()), hb.quant_mx4(torch.from_numpy(w).cuda())
+        _check_product(hb.gemm_mx4(qa, qw), mx4_ref.held(x), mx4_ref.held(w), None, F32)
+        tiny = np.float32(2.0 ** -63)
+        qa, qw = hb.quant_mx4(torch.from_numpy(np.sign(x) * tiny).cuda()), hb.quant_mx4(torch.from_numpy(np.sign(w) * tiny).cuda())
+        _check_product(hb.gemm_mx4(qa, qw), np.sign(x) * float(tiny), np.sign(w) * float(tiny), None, F32)
+
+
+@pytest.mark.parametrize("m", [2, 12, 60, 300])
+def test_a_bad_block_spoils_its_row_and_no_other(hb, m):
+    rng = np.random.default_rng(m)
+    x, w = _rand(rng, m, 600, F32), _rand(rng, 90, 600, F32)
+    x[1, 599], w[7, 0] = float("inf"), float("nan")
+    y = _np(hb.linear_mx4(x, hb.quant_mx4(w)))
+    want = np.zeros(y.shape, dtype=bool)
+    want[1], want[:, 7] = True, True
+    np.testing.assert_array_equal(np.isnan(y), want)
+
+
+def test_rows_behind_the_last_may_hold_anything(hb):
+    """Scale rows between `rows` and the next multiple of 16 are nobody's."""
+    rng = np.random.default_rng(11)
+    for m, n in ((5, 20), (40, 33), (130, 140)):
+        a, b = hb.quant_mx4(_rand(rng, m, 500, F32)), hb.quant_mx4(_rand(rng, n, 500, F32))
+        want = hb.gemm_mx4(a, b)
+        for t in (a, b):
+            t.scales[:, t.desc.rows:] = 255
+        assert torch.equal(hb.gemm_mx4(a, b), want)
+
+
+@pytest.mark.parametrize("tokens,features,outputs,dtype", [(1, 40, 70, F32), (37, 300, 130, BF16), (500, 730, 1100, F32), (260, 512, 520, F16)])
+def test_a_training_step(hb, tokens, features, outputs, dtype):
+    """Forward product and both gradients, each from the operands that one read of every matrix gives."""
+    rng = np.random.default_rng(tokens)
+    x, w, dy = _rand(rng, tokens, features, dtype, 1), _rand(rng, outputs, features, dtype, 1), _rand(rng, tokens, outputs, dtype, 1)
+    (xa, xd), (wa, wd), (ga, gd) = hb.quant_mx4_both(x), hb.quant_mx4_both(w), hb.quant_mx4_both(dy, hb.STOCHASTIC, 5)
+    h = mx4_ref.words(tokens, outputs, 5)
+    _check_product(hb.gemm_mx4(xa, wa, dtype=dtype), mx4_ref.held(_np(x)), mx4_ref.held(_np(w)), None, dtype)
+    _check_product(hb.gemm_mx4(ga, wd, dtype=dtype), mx4_ref.held(_np(dy), h), mx4_ref.held(_np(w).T), None, dtype)
+    _check_product(hb.gemm_mx4(gd, xd), mx4_ref.held(_np(dy).T, h.T), mx4_ref.held(_np(x).T), None, F32)
+
+
+def test_columns_of_one_matrix(hb):
+    """x and y side by side in one buffer, at every size class."""
+    rng = np.random.default_rng(4)
+    w = _rand(rng, 96, 320, BF16, 1)
+    qw = hb.quant_mx4(w)
+    for m in (1, 2, 9, 200):
+        both = torch.zeros((m, 320 + 96), dtype=BF16, device="cuda")
+        both[:, :320] = _rand(rng, m, 320, BF16, 1)
+        x = both[:, :320].clone()
+        hb.linear_mx4(both[:, :320], qw, out=both[:, 320:])
+        assert torch.equal(both[:, :320], x) and torch.equal(both[:, 320:], hb.linear_mx4(x, qw))
+
+
+def test_on_another_stream_and_in_a_graph(hb):
+    """A training step captured once and replayed on new inputs, with the program's own work between the replays."""
+    rng = np.random.default_rng(6)
+    x, w, dy = (torch.empty(s, device="cuda") for s in ((300, 700), (520, 700), (300, 520)))
+
+    def step():
+        (xa, xd), (wa, wd), (ga, gd) = hb.quant_mx4_both(x), hb.quant_mx4_both(w), hb.quant_mx4_both(dy, hb.STOCHASTIC, 5)
+        return hb.gemm_mx4(xa, wa), hb.gemm_mx4(ga, wd), hb.gemm_mx4(gd, xd), hb.linear_mx4(x[:1], wa)
+
+    def fill(seed):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        for t in (x, w, dy):
+            t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+    fill(0)
+    want = step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = step()
+    y = hb.linear_mx4(x, hb.quant_mx4(w, stream=side), stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(y, want[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for seed in (1, 2, 3, 4):
+        fill(seed)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, step()))
+    del rng
