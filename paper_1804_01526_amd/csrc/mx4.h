@@ -72,17 +72,19 @@ __device__ __forceinline__ uint32_t mx4_codes8(const float *x, uint32_t byte) {
     return byte == 255u ? 0u : w;
 }
 
-// ... stochastically.  |x| in units is exact in FP32 (but for values that vanish); a step is 1/2, 1 or 2 units, and q steps are the code q,
-// q + 2 and q + 4.  The fraction of a step times 2^32, cut to an integer, decides as the exact one does: h is an integer.
-__device__ __forceinline__ uint32_t mx4_code_sr(float x, int neg_exp, uint32_t h) {
-    const float a = __builtin_amdgcn_ldexpf(__builtin_fabsf(x), neg_exp);
-    const int up = a < 2.0f ? 0 : a < 4.0f ? 1 : 2;
-    const float t = __builtin_amdgcn_ldexpf(a, 1 - up);
-    const uint32_t whole = (uint32_t)t;
-    const uint32_t frac = (uint32_t)__builtin_amdgcn_ldexpf(__builtin_amdgcn_fractf(t), 32);
-    uint32_t code = whole + ((frac + h) < h ? 1u : 0u) + 2u * (uint32_t)up;
+// ... stochastically.  From two units up a step is the second bit of the significand, whatever the exponent, so that the code is the upper bits of
+// the number itself after the word's top 22 bits are added below; exponent and bit count the codes from 4 on.  Below, a step is half a unit: the
+// fraction of 2 |x| times 2^32, cut to an integer, decides as the exact one does, h being an integer.  (What |x| in units loses when it leaves
+// FP32's range is far below 2^-32.)
+__device__ __forceinline__ uint32_t mx4_code_sr(float x, uint32_t byte, uint32_t h) {
+    const uint32_t bits = __float_as_uint(x) & 0x7fffffffu;
+    const uint32_t high = ((bits + (h >> 10)) >> 22) + 2u - 2u * byte;
+    const float a = __builtin_amdgcn_ldexpf(__builtin_fabsf(x), 128 - (int)byte);
+    const uint32_t frac = (uint32_t)__builtin_amdgcn_ldexpf(__builtin_amdgcn_fractf(a), 32);
+    const uint32_t low = (uint32_t)a + ((frac + h) < h ? 1u : 0u);
+    uint32_t code = a >= 4.0f ? high : low;
     code = code > 7u ? 7u : code;
-    return code | (__float_as_uint(x) >> 31) << 3;
+    return code | ((__float_as_uint(x) >> 28) & 8u);
 }
 
 // largest magnitude of eight values, as bits (a NaN is larger than everything)

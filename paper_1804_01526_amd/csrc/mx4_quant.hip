@@ -22,7 +22,7 @@ __device__ __forceinline__ uint32_t codes8(const float *x, uint32_t byte, int64_
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint64_t at = (uint64_t)idx + i;
-            w |= mx4_code_sr(x[i], 127 - (int)byte, sr_hash((uint32_t)at, (uint32_t)(at >> 32), p.s0, p.s1)) << (4 * i);
+            w |= mx4_code_sr(x[i], byte, sr_hash((uint32_t)at, (uint32_t)(at >> 32), p.s0, p.s1)) << (4 * i);
         }
         return byte == 255u ? 0u : w;
     }
@@ -53,111 +53,89 @@ __global__ __launch_bounds__(256) void quant_mx4_along_kernel(const QuantMx4Para
     }
 }
 
-// ---- down the columns, or both.  A workgroup has a tile of 128 x 128: it converts along the rows from the registers that the values were
-// loaded into, and down the columns from LDS, where a thread reads two neighbouring columns of 32 rows (a wave reads whole rows).
-template <int DT>
-struct Tile {
-    static constexpr int kSize = DT == HBFP_F32 ? 4 : 2;
-    static constexpr int kBytes = 128 * 128 * kSize;
-};
+// ---- down the columns, or both.  A workgroup has a tile of 128 x 128, a thread 8 x 8 of it: four neighbouring lanes share the blocks along
+// its rows, and the four lanes 16 apart of a wave those down its columns, so that both maxima are found between lanes and a random word serves both
+// codes of its value.  The words of the columns meet in LDS, from where four threads store 64 bytes of a column's codes.
+// largest of the lanes l, l ^ 16, l ^ 32, l ^ 48: two exchanges of rows of lanes on the vector unit
+__device__ __forceinline__ uint32_t largest_of_column(uint32_t x) {
+    const v2u a = __builtin_bit_cast(v2u, __builtin_amdgcn_permlane32_swap(x, x, false, false));
+    x = a[0] > a[1] ? a[0] : a[1];
+    const v2u b = __builtin_bit_cast(v2u, __builtin_amdgcn_permlane16_swap(x, x, false, false));
+    return b[0] > b[1] ? b[0] : b[1];
+}
+
 template <int DT, int ROUND, bool ALONG>
-__global__ __launch_bounds__(256) void quant_mx4_down_kernel(const QuantMx4Params p) {
-    extern __shared__ __attribute__((aligned(16))) uint8_t tile[];
-    const int t = threadIdx.x;
+__global__ __launch_bounds__(256, ALONG && ROUND == HBFP_STOCHASTIC ? 3 : 4) void quant_mx4_down_kernel(const QuantMx4Params p) {
+    __shared__ __attribute__((aligned(16))) uint32_t words[128][20];     // 16 of column 8 a + b in row 16 b + a: a wave's writes cover all banks
+    const int t = threadIdx.x, lane = t & 63, tr = t / 16;
     const int64_t c0 = (int64_t)(blockIdx.x % p.tiles_c) * 128, r0 = (int64_t)(blockIdx.x / p.tiles_c) * 128;
-    {
-        const int64_t c = c0 + 8 * (t % 16), left = p.cols - c;
-        float x[8][8];
+    const int64_t c = c0 + 8 * (t % 16), r = r0 + 8 * tr, left = p.cols - c;
+    float x[8][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t r = r0 + t / 16 + 16 * i;
-            load8<DT>(p.src, r * p.ld + c, r >= p.rows || left <= 0 ? 0 : left < 8 ? (int)left : 8, x[i]);
-        }
+    for (int i = 0; i < 8; ++i) load8<DT>(p.src, (r + i) * p.ld + c, r + i >= p.rows || left <= 0 ? 0 : left < 8 ? (int)left : 8, x[i]);
+    uint32_t down[8];                                       // bytes of the columns' blocks
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int at = (t / 16 + 16 * i) * 128 + 8 * (t % 16);
-            if constexpr (DT == HBFP_F32) {
-                v4f *to = reinterpret_cast<v4f *>(tile + 4 * at);
-                to[0] = v4f{x[i][0], x[i][1], x[i][2], x[i][3]};
-                to[1] = v4f{x[i][4], x[i][5], x[i][6], x[i][7]};
-            } else {
-                uint32_t w[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if constexpr (DT == HBFP_BF16) w[k] = __float_as_uint(x[i][2 * k]) >> 16 | (__float_as_uint(x[i][2 * k + 1]) & 0xffff0000u);
-                    else
-                        w[k] = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x[i][2 * k]) |
-                               (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x[i][2 * k + 1]) << 16;
-                }
-                *reinterpret_cast<v4u *>(tile + 2 * at) = v4u{w[0], w[1], w[2], w[3]};
-            }
-        }
-        if constexpr (ALONG) {
-            const int64_t group = c0 >> 8;
-            if (group < p.along.groups) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int64_t r = r0 + t / 16 + 16 * i;
-                    const uint32_t byte = mx4_byte<ROUND>(largest_of_quad(mx4_largest8(x[i])));
-                    const uint32_t w = codes8<ROUND>(x[i], byte, r * p.cols + c, p);
-                    if (r >= p.rows) continue;
-                    reinterpret_cast<uint32_t *>(p.along.codes + (group * p.rows + r) * 128 + ((c0 & 255) >> 1))[t % 16] = w;
-                    if (t % 4 == 0) p.along.scales[(group * p.along.scale_rows + r) * 8 + ((c0 & 255) >> 5) + (t % 16) / 4] = (uint8_t)byte;
-                }
-            }
-        }
-    }
-    __syncthreads();
-    const int64_t k0 = r0 + 32 * (t / 64), group = k0 >> 8;          // (a wave has one block of 32 rows)
-    if (group >= p.down.groups) return;
-    const int cc = 2 * (t % 64);
-    float x[2][32];
-    const uint8_t *from = tile + ((t / 64) * 32 * 128 + cc) * Tile<DT>::kSize;
-#pragma unroll
-    for (int k = 0; k < 32; ++k) {
-        if constexpr (DT == HBFP_F32) {
-            const v2f two = *reinterpret_cast<const v2f *>(from + k * 512);
-            x[0][k] = two[0];
-            x[1][k] = two[1];
-        } else {
-            const uint32_t two = *reinterpret_cast<const uint32_t *>(from + k * 256);
-            if constexpr (DT == HBFP_BF16) {
-                x[0][k] = __uint_as_float(two << 16);
-                x[1][k] = __uint_as_float(two & 0xffff0000u);
-            } else {
-                x[0][k] = (float)__builtin_bit_cast(_Float16, (uint16_t)two);
-                x[1][k] = (float)__builtin_bit_cast(_Float16, (uint16_t)(two >> 16));
-            }
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int64_t c = c0 + cc + j;
-        if (c >= p.cols) continue;
+    for (int j = 0; j < 8; ++j) {
         uint32_t amax = 0;
 #pragma unroll
-        for (int k = 0; k < 32; k += 8) {
-            const uint32_t a = mx4_largest8(x[j] + k);
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t a = __float_as_uint(x[i][j]) & 0x7fffffffu;
             amax = a > amax ? a : amax;
         }
-        const uint32_t byte = mx4_byte<ROUND>(amax);
-        v4u w;
+        down[j] = mx4_byte<ROUND>(largest_of_column(amax));
+    }
+    uint32_t column[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if constexpr (ROUND == HBFP_RNE) {
-                w[k] = mx4_codes8(x[j] + 8 * k, byte);
-            } else {
-                w[k] = 0;
+    for (int i = 0; i < 8; ++i) {
+        // one row after the other: side by side they would take 256 registers
+        __builtin_amdgcn_sched_barrier(0);
+        uint64_t at = (uint64_t)(r + i) * (uint64_t)p.cols + (uint64_t)c;
+        asm volatile("" : "+v"(at));
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint64_t at = (uint64_t)(k0 + 8 * k + i) * (uint64_t)p.cols + (uint64_t)c;
-                    w[k] |= mx4_code_sr(x[j][8 * k + i], 127 - (int)byte, sr_hash((uint32_t)at, (uint32_t)(at >> 32), p.s0, p.s1)) << (4 * i);
-                }
-                if (byte == 255u) w[k] = 0;
+        for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(x[i][j]));
+        uint32_t byte = 0, w = 0;
+        if constexpr (ALONG) byte = mx4_byte<ROUND>(largest_of_quad(mx4_largest8(x[i])));
+        if constexpr (ROUND == HBFP_RNE) {
+            if constexpr (ALONG) w = mx4_codes8(x[i], byte);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j, ++at) {
+                const uint32_t h = sr_hash((uint32_t)at, (uint32_t)(at >> 32), p.s0, p.s1);
+                if constexpr (ALONG) w |= mx4_code_sr(x[i][j], byte, h) << (4 * j);
+                column[j] |= mx4_code_sr(x[i][j], down[j], h) << (4 * i);
+            }
+            if (byte == 255u) w = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(column[j]));
+            asm volatile("" : "+v"(w));
+        }
+        if constexpr (ALONG) {
+            if (r + i < p.rows) {
+                const int64_t line = (c0 >> 8) * p.rows + r + i;
+                reinterpret_cast<uint32_t *>(p.along.codes + line * 128 + ((c0 & 255) >> 1))[t % 16] = w;
+                if (t % 4 == 0) p.along.scales[((c0 >> 8) * p.along.scale_rows + r + i) * 8 + ((c0 & 255) >> 5) + (t % 16) / 4] = (uint8_t)byte;
             }
         }
-        *reinterpret_cast<v4u *>(p.down.codes + (group * p.cols + c) * 128 + ((k0 & 255) >> 1)) = w;
-        p.down.scales[(group * p.down.scale_rows + c) * 8 + ((k0 & 255) >> 5)] = (uint8_t)byte;
+    }
+    const int64_t group = r0 >> 8;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (ROUND == HBFP_RNE) {
+            const float y[8] = {x[0][j], x[1][j], x[2][j], x[3][j], x[4][j], x[5][j], x[6][j], x[7][j]};
+            column[j] = mx4_codes8(y, down[j]);
+        } else {
+            if (down[j] == 255u) column[j] = 0;
+        }
+        words[16 * j + t % 16][tr] = column[j];
+        if (lane < 16 && c + j < p.cols) p.down.scales[(group * p.down.scale_rows + c + j) * 8 + ((r0 & 255) >> 5) + t / 64] = (uint8_t)down[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int col = 64 * i + t / 4;
+        if (c0 + col < p.cols)
+            *reinterpret_cast<v4u *>(p.down.codes + (group * p.cols + c0 + col) * 128 + ((r0 & 255) >> 1) + 16 * (t % 4)) =
+                *reinterpret_cast<const v4u *>(&words[16 * (col % 8) + col / 8][4 * (t % 4)]);
     }
 }
 
@@ -176,9 +154,7 @@ int launch_quant(QuantMx4Params p, bool along, bool down, hipStream_t s) {
     if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
     p.tiles_c = (uint32_t)tiles_c;
     void (*const kernel)(QuantMx4Params) = along ? &quant_mx4_down_kernel<DT, ROUND, true> : &quant_mx4_down_kernel<DT, ROUND, false>;
-    static std::atomic<bool> configured[2];
-    if (allow_dynamic_lds(configured[along], reinterpret_cast<const void *>(kernel), Tile<DT>::kBytes) != HBFP_OK) return HBFP_ERR_LAUNCH;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), Tile<DT>::kBytes, s, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), 0, s, p);
     return launch_status();
 }
 

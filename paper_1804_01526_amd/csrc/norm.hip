@@ -217,12 +217,46 @@ int launch_type(const NormArgs &a, hipStream_t s) {
 
 // ---- the gradient.  With u = sum * rstd:  dx = g_sum + rstd (g w - u mean(g w u)),  dweight = sum over rows of g u.
 // A workgroup takes rows wg, wg + G, ... and its threads keep their columns: weight and the sums of dweight stay in registers, and
-// each row is read once.  The partial sums of the G workgroups are added in their order by a second kernel.
+// each row is read once, the next one's while this one is worked on (AHEAD).  The partial sums of the G workgroups are added in their
+// order by a second kernel.
 struct GradParams {
     NormGradArgs a;
     int32_t wgs;
 };
-template <int DT, int W, int KEEP>
+
+// eight consecutive elements as they lie in memory; of which n (may be <= 0) exist, the others 0
+template <int DT>
+struct Raw8 {
+    static constexpr int kWords = DT == HBFP_F32 ? 8 : 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const void *p, int64_t i, int n) {
+        typedef uint32_t words_at __attribute__((ext_vector_type(4), aligned(2)));
+        if (n >= 8) {
+#pragma unroll
+            for (int k = 0; k < kWords / 4; ++k) {
+                const words_at x = *reinterpret_cast<const words_at *>(reinterpret_cast<const uint8_t *>(p) + i * (kWords / 2) + 16 * k);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[4 * k + j] = x[j];
+            }
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) w[k] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) {
+                if constexpr (DT == HBFP_F32) w[j] = reinterpret_cast<const uint32_t *>(p)[i + j];
+                else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[i + j] << (16 * (j & 1));
+            }
+    }
+    __device__ __forceinline__ float get(int j) const {
+        if constexpr (DT == HBFP_F32) return __uint_as_float(w[j]);
+        const uint32_t h = j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu;
+        return DT == HBFP_BF16 ? __uint_as_float(h << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)h);
+    }
+};
+
+template <int DT, int W, int KEEP, bool AHEAD>
 __global__ __launch_bounds__(64 * W) void norm_grad_kernel(const GradParams p) {
     __shared__ float meet[2][W];
     const NormGradArgs &a = p.a;
@@ -242,27 +276,39 @@ __global__ __launch_bounds__(64 * W) void norm_grad_kernel(const GradParams p) {
             dw[i][k] = 0.0f;
         }
     }
-    int turn = 0;
-    const float inv = 1.0f / (float)a.cols;
-    for (int64_t row = blockIdx.x; row < a.rows; row += p.wgs, turn ^= 1) {
-        float g[KEEP][8], s[KEEP][8], o[KEEP][8];
+    Raw8<DT> g[KEEP], s[KEEP], o[KEEP];
+    float r = 0.0f;
+    const auto request = [&](int64_t row) {
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) {
-            load8<DT>(a.g, row * a.ldg + c0 + kStep * i, left[i], g[i]);
-            load8<DT>(a.sum, row * a.ld_sum + c0 + kStep * i, left[i], s[i]);
-            if (a.g_sum) load8<DT>(a.g_sum, row * a.ld_g_sum + c0 + kStep * i, left[i], o[i]);
+            g[i].load(a.g, row * a.ldg + c0 + kStep * i, left[i]);
+            s[i].load(a.sum, row * a.ld_sum + c0 + kStep * i, left[i]);
+            if (a.g_sum) o[i].load(a.g_sum, row * a.ld_g_sum + c0 + kStep * i, left[i]);
         }
-        const float r = a.rstd[row];
+        r = a.rstd[row];
+    };
+    const float inv = 1.0f / (float)a.cols;
+    int turn = 0;
+    if (AHEAD) request(blockIdx.x);
+    for (int64_t row = blockIdx.x; row < a.rows; row += p.wgs, turn ^= 1) {
+        if (!AHEAD) request(row);
+        float u[KEEP][8], v[KEEP][8];
         float dot = 0.0f;
+        const float rr = r;
 #pragma unroll
         for (int i = 0; i < KEEP; ++i)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float u = s[i][k] * r, gu = g[i][k] * u;
-                dw[i][k] += gu;
-                dot = __builtin_fmaf(gu, weight[i][k], dot);
-                s[i][k] = u;
+                const float gk = g[i].get(k);
+                u[i][k] = s[i].get(k) * rr;
+                v[i][k] = gk * weight[i][k];
+                dw[i][k] = __builtin_fmaf(gk, u[i][k], dw[i][k]);
+                dot = __builtin_fmaf(v[i][k], u[i][k], dot);
             }
+        Raw8<DT> other[KEEP];
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) other[i] = o[i];
+        if (AHEAD && row + p.wgs < a.rows) request(row + p.wgs);
         dot = over_row<W>(dot, meet[turn], wave, lane, Add());      // (two rooms: the next row's may be written while this one is read)
         const float mean = dot * inv;
 #pragma unroll
@@ -270,8 +316,8 @@ __global__ __launch_bounds__(64 * W) void norm_grad_kernel(const GradParams p) {
             float d[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float v = __builtin_fmaf(-s[i][k], mean, g[i][k] * weight[i][k]);
-                d[k] = a.g_sum ? __builtin_fmaf(r, v, o[i][k]) : r * v;
+                const float e = __builtin_fmaf(-u[i][k], mean, v[i][k]);
+                d[k] = a.g_sum ? __builtin_fmaf(rr, e, other[i].get(k)) : rr * e;
             }
             store8<DT>(a.dx, row * a.ldx + c0 + kStep * i, left[i], d);
         }
@@ -340,52 +386,57 @@ __global__ __launch_bounds__(256) void norm_dweight_kernel(const GradParams p) {
     store8<HBFP_F32>(a.partial, (int64_t)blockIdx.y * a.cols + c, left, dw);
 }
 
-// dweight from the partial sums: a workgroup has 64 columns; each of its four waves adds a quarter of the G sums, in their order
-__global__ __launch_bounds__(256) void norm_dweight_sum_kernel(const GradParams p) {
-    __shared__ float meet[4][64];
+// dweight from the partial sums: a workgroup has 32 columns, its 32 half waves a share of the G sums each; both steps add in order
+constexpr int kShares = 32;
+__global__ __launch_bounds__(32 * kShares) void norm_dweight_sum_kernel(const GradParams p) {
+    __shared__ float meet[kShares][32];
     const NormGradArgs &a = p.a;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-    const int per = (p.wgs + 3) / 4, end = (wave + 1) * per < p.wgs ? (wave + 1) * per : p.wgs;
+    const int lane = threadIdx.x & 31, share = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    const int per = (p.wgs + kShares - 1) / kShares, end = (share + 1) * per < p.wgs ? (share + 1) * per : p.wgs;
     float sum = 0.0f;
     if (c < a.cols)
-        for (int i = wave * per; i < end; i += 8) {
+        for (int i = share * per; i < end; i += 8) {
             float v[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = i + k < end ? a.partial[(int64_t)(i + k) * a.cols + c] : 0.0f;
 #pragma unroll
             for (int k = 0; k < 8; ++k) sum += v[k];
         }
-    meet[wave][lane] = sum;
+    meet[share][lane] = sum;
     __syncthreads();
-    if (wave == 0 && c < a.cols) a.dweight[c] = ((meet[0][lane] + meet[1][lane]) + meet[2][lane]) + meet[3][lane];
+    if (share > 0 || c >= a.cols) return;
+    for (int i = 1; i < kShares; ++i) sum += meet[i][lane];
+    a.dweight[c] = sum;
 }
 
 constexpr int64_t kGradKept = 16384;
 // workgroups that share the rows: enough to keep the memory busy, each with rows enough for its partial sums not to matter
 int64_t grad_wgs(int64_t rows, int64_t cols) {
-    const int64_t most = cols > kGradKept ? 64 : cols > 4096 ? 256 : 512;
+    const int64_t waves = cols <= 512 ? 1 : cols <= 1024 ? 2 : cols <= 2048 ? 4 : cols <= 4096 ? 8 : 16;
+    const int64_t most = cols > kGradKept ? 64 : 4096 / waves;
     return rows < most ? rows : most;
 }
 
-template <int DT, int W, int KEEP>
+template <int DT, int W, int KEEP, bool AHEAD>
 void launch_grad_rows(const GradParams &p, hipStream_t s) {
-    hipLaunchKernelGGL((norm_grad_kernel<DT, W, KEEP>), dim3((unsigned)p.wgs), dim3(64 * W), 0, s, p);
+    hipLaunchKernelGGL((norm_grad_kernel<DT, W, KEEP, AHEAD>), dim3((unsigned)p.wgs), dim3(64 * W), 0, s, p);
 }
 template <int DT>
 int launch_grad(const NormGradArgs &a, hipStream_t s) {
     const GradParams p = {a, (int32_t)grad_wgs(a.rows, a.cols)};
-    if (a.cols <= 512) launch_grad_rows<DT, 1, 1>(p, s);
-    else if (a.cols <= 2048) launch_grad_rows<DT, 4, 1>(p, s);
-    else if (a.cols <= 4096) launch_grad_rows<DT, 4, 2>(p, s);
-    else if (a.cols <= 8192) launch_grad_rows<DT, 8, 2>(p, s);
-    else if (a.cols <= kGradKept) launch_grad_rows<DT, 16, 2>(p, s);
+    if (a.cols <= 512) launch_grad_rows<DT, 1, 1, true>(p, s);
+    else if (a.cols <= 1024) launch_grad_rows<DT, 2, 1, true>(p, s);
+    else if (a.cols <= 2048) launch_grad_rows<DT, 4, 1, true>(p, s);
+    else if (a.cols <= 4096) launch_grad_rows<DT, 8, 1, true>(p, s);
+    else if (a.cols <= 8192) launch_grad_rows<DT, 16, 1, true>(p, s);
+    else if (a.cols <= kGradKept) launch_grad_rows<DT, 16, 2, false>(p, s);
     else {
         // (dx may be written over g)
         if (a.dweight) hipLaunchKernelGGL(norm_dweight_kernel<DT>, dim3((unsigned)ceil_div(a.cols, 2048), (unsigned)p.wgs), dim3(256), 0, s, p);
         hipLaunchKernelGGL(norm_grad_long_kernel<DT>, dim3((unsigned)a.rows), dim3(1024), 0, s, a);
     }
-    if (a.dweight) hipLaunchKernelGGL(norm_dweight_sum_kernel, dim3((unsigned)ceil_div(a.cols, 64)), dim3(256), 0, s, p);
+    if (a.dweight) hipLaunchKernelGGL(norm_dweight_sum_kernel, dim3((unsigned)ceil_div(a.cols, 32)), dim3(32 * kShares), 0, s, p);
     return launch_status();
 }
 
