@@ -2,6 +2,8 @@
 //     y[m][n] = sum over blocks of 32 of 2^(sa + sb - 254) * (sum of the block's products) + bias[n]
 // on v_mfma_scale_f32_*_f8f6f4 with both operands in 4 bits: a lane hands the instruction one block, 32 codes in 16 bytes as they
 // are stored, and its scale byte, and the instruction multiplies, scales and accumulates in FP32.
+#include <math.h>
+
 #include "gemm_wide.h"
 #include "mx4.h"
 
@@ -37,7 +39,7 @@ struct Mx4Tile {
 };
 
 template <int T, int RING, int OUT, bool STREAM>
-__global__ __launch_bounds__(256, T == 4 ? 1 : 2) void gemm_mx4_kernel(const Mx4Params p) {
+__global__ __launch_bounds__(256, T > 2 ? 1 : T == 2 ? 2 : 4) void gemm_mx4_kernel(const Mx4Params p) {
     typedef Mx4Tile<T, RING> W;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const Mx4Product &q = p.q;
@@ -116,39 +118,38 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void gemm_mx4_kernel(const Mx4
 
     v4i a[2][T], b[2][T];                               // [buffer][tile]
     int as[2][T], bs[2][T];                             // scale words of this stage and of the next
+    // request r of a k-step's fragments, in the order in which its matrix instructions want them: row tile 0, all column tiles, the other row tiles
+#define HBFP_MX4_READ(buf, base_, s, r)                                                                        \
+    {                                                                                                         \
+        if ((r) == 0 || (r) > T) a[buf][(r) ? (r) - T : 0] = *reinterpret_cast<const v4i *>((base_) + fa[s] + ((r) ? (r) - T : 0) * 32 * 128); \
+        else b[buf][(r) - 1] = *reinterpret_cast<const v4i *>((base_) + fb[s] + ((r) - 1) * 32 * 128);        \
+    }
+#define HBFP_MX4_READ_SCALE(buf, base_, r)                                                                     \
+    {                                                                                                         \
+        if ((r) == 0 || (r) > T) as[buf][(r) ? (r) - T : 0] = *reinterpret_cast<const int *>((base_) + ga + ((r) ? (r) - T : 0) * 32 * 8); \
+        else bs[buf][(r) - 1] = *reinterpret_cast<const int *>((base_) + gb + ((r) - 1) * 32 * 8);            \
+    }
 #define HBFP_MX4_FENCE                  \
     asm volatile("" ::: "memory");      \
     __builtin_amdgcn_sched_barrier(0)
-#define HBFP_MX4_READ(buf, base_, s, i)                                                                        \
-    {                                                                                                         \
-        a[buf][i] = *reinterpret_cast<const v4i *>((base_) + fa[s] + (i) * 32 * 128);                         \
-        b[buf][i] = *reinterpret_cast<const v4i *>((base_) + fb[s] + (i) * 32 * 128);                         \
-    }
-#define HBFP_MX4_READ_SCALES(buf, base_, i)                                                                    \
-    {                                                                                                         \
-        as[buf][i] = *reinterpret_cast<const int *>((base_) + ga + (i) * 32 * 8);                             \
-        bs[buf][i] = *reinterpret_cast<const int *>((base_) + gb + (i) * 32 * 8);                             \
-    }
-#define HBFP_MX4_ROW(buf, s, i)                                                                                \
-    {                                                                                                         \
-        _Pragma("unroll") for (int j = 0; j < T; ++j)                                                         \
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(four_bit(a[buf][i]), four_bit(b[buf][j]), acc[i][j], 4, 4, s, \
-                                                                        as[0][i], s, bs[0][j]);               \
-    }
-    // one k-step of 64: T x T matrix instructions on buffer `buf`; after each row of them, one row tile and one column tile of the next
-    // k-step are requested into the other buffer
+#define HBFP_MX4_MFMA(buf, s, i, j)                                                                            \
+    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(four_bit(a[buf][i]), four_bit(b[buf][j]), acc[i][j], 4, 4, s, as[0][i], s, bs[0][j])
+    // one k-step of 64: T x T matrix instructions on one buffer, and behind the first of them, one by one, the requests of the next k-step's
+    // fragments into the other: what stands behind a matrix instruction issues while it runs
 #define HBFP_MX4_KSTEP(s, base_)                                                                               \
     {                                                                                                         \
-        _Pragma("unroll") for (int i_ = 0; i_ < T; ++i_) {                                                    \
-            HBFP_MX4_ROW((s) & 1, s, i_);                                                                     \
-            HBFP_MX4_READ(1 - ((s) & 1), base_, (s) + 1, i_);                                                 \
+        constexpr int per_ = (2 * T + T * T - 1) / (T * T);                                                   \
+        _Pragma("unroll") for (int e_ = 0; e_ < T * T; ++e_) {                                                \
+            HBFP_MX4_MFMA((s) & 1, s, e_ / T, e_ % T);                                                        \
+            _Pragma("unroll") for (int r_ = e_ * per_; r_ < (e_ + 1) * per_ && r_ < 2 * T; ++r_)              \
+                HBFP_MX4_READ(1 - ((s) & 1), base_, (s) + 1, r_);                                             \
             HBFP_MX4_FENCE;                                                                                   \
         }                                                                                                     \
     }
     // A stage is four k-steps; the fragments of its first, and its scale words, were requested during the stage before.  The hand-over,
-    // in its last: this wave has its last fragments of the stage, and its copies of the next stage have landed when only those of the
-    // AFTER stages behind it are in flight; after the barrier that holds for everybody, and the buffer takes the copies of stage st + RING
-    // (COPY).  LAST: nothing follows.
+    // behind the second matrix instruction of its last: this wave has its last fragments of the stage, and its copies of the next stage have
+    // landed when only those of the AFTER stages behind it are in flight; after the barrier that holds for everybody, and the buffer takes the
+    // copies of stage st + RING (COPY), spread over the rest of the k-step.  LAST: nothing follows.
 #define HBFP_MX4_STAGE(AFTER, COPY, LAST)                                                                      \
     {                                                                                                         \
         const uint8_t *base = lds + ring * W::kStage;                                                         \
@@ -157,19 +158,23 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void gemm_mx4_kernel(const Mx4
         HBFP_MX4_KSTEP(0, base);                                                                              \
         HBFP_MX4_KSTEP(1, base);                                                                              \
         HBFP_MX4_KSTEP(2, base);                                                                              \
-        _Pragma("unroll") for (int i_ = 0; i_ < T; ++i_) {                                                    \
-            HBFP_MX4_ROW(1, 3, i_);                                                                           \
-            if (!(LAST)) {                                                                                    \
-                if (i_ == 0) {                                                                                \
+        constexpr int hand_ = T > 1 ? 1 : 0, slots_ = T * T - hand_, per_ = (2 * T + slots_ - 1) / slots_;    \
+        _Pragma("unroll") for (int e_ = 0; e_ < T * T; ++e_) {                                                \
+            HBFP_MX4_MFMA(1, 3, e_ / T, e_ % T);                                                              \
+            if (!(LAST) && e_ >= hand_) {                                                                     \
+                if (e_ == hand_) {                                                                            \
                     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((AFTER) * (W::kCopies + 1)) : "memory"); \
                     __builtin_amdgcn_s_barrier();                                                             \
                     asm volatile("" ::: "memory");                                                            \
                 }                                                                                             \
-                HBFP_MX4_READ(0, nbase, 0, i_);                                                               \
-                HBFP_MX4_READ_SCALES(1, nbase, i_);                                                           \
+                _Pragma("unroll") for (int r_ = (e_ - hand_) * per_; r_ < (e_ - hand_ + 1) * per_ && r_ < 2 * T; ++r_) { \
+                    HBFP_MX4_READ(0, nbase, 0, r_);                                                           \
+                    HBFP_MX4_READ_SCALE(1, nbase, r_);                                                        \
+                }                                                                                             \
                 if (COPY) {                                                                                   \
-                    _Pragma("unroll") for (int c_ = 0; c_ < W::kCopies / T; ++c_) HBFP_MX4_COPY(W::kCopies / T * i_ + c_, ring); \
-                    if (i_ == T - 1) HBFP_MX4_COPY_LAST(ring);                                                \
+                    _Pragma("unroll") for (int c_ = (e_ - hand_) * W::kCopies / slots_; c_ < (e_ - hand_ + 1) * W::kCopies / slots_; ++c_) \
+                        HBFP_MX4_COPY(c_, ring);                                                              \
+                    if (e_ == T * T - 1) HBFP_MX4_COPY_LAST(ring);                                            \
                 }                                                                                             \
             }                                                                                                 \
             HBFP_MX4_FENCE;                                                                                   \
@@ -196,11 +201,12 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void gemm_mx4_kernel(const Mx4
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < T; ++i) {
-        HBFP_MX4_READ(0, lds, 0, i);
-        HBFP_MX4_READ_SCALES(0, lds, i);
-        as[1][i] = bs[1][i] = 0;
+    for (int r = 0; r < 2 * T; ++r) {
+        HBFP_MX4_READ(0, lds, 0, r);
+        HBFP_MX4_READ_SCALE(0, lds, r);
     }
+#pragma unroll
+    for (int i = 0; i < T; ++i) as[1][i] = bs[1][i] = 0;
     __builtin_amdgcn_sched_barrier(0);
     if (RING > 3 && nstage > 3) HBFP_MX4_COPY_STAGE(3);
     int ring = 0;
@@ -218,8 +224,8 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void gemm_mx4_kernel(const Mx4
     HBFP_MX4_STAGE(0, false, true);
 #undef HBFP_MX4_STAGE
 #undef HBFP_MX4_KSTEP
-#undef HBFP_MX4_ROW
-#undef HBFP_MX4_READ_SCALES
+#undef HBFP_MX4_MFMA
+#undef HBFP_MX4_READ_SCALE
 #undef HBFP_MX4_READ
 #undef HBFP_MX4_FENCE
 #undef HBFP_MX4_COPY_STAGE
@@ -227,7 +233,7 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void gemm_mx4_kernel(const Mx4
 #undef HBFP_MX4_COPY
 
     const int64_t i0 = row0 + 32 * T * wm, j0 = col0 + 32 * T * wn;
-    if (T == 2 && p.splits > 1) {
+    if (T == 1 && p.splits > 1) {
         store_result<T, T, false>(p.partial + ((int64_t)split * M + i0) * N + j0, N, M - i0, N - j0, false, lane,
                                   [&](int i, int j, int v) { return acc[i][j][v]; });
         return;
@@ -242,8 +248,7 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void gemm_mx4_kernel(const Mx4
     const auto value = [&](int i, int j, int v) { return has_bias ? acc[i][j][v] + bias[j] : acc[i][j][v]; };
     if constexpr (OUT == kWideF32) store_result<T, T, STREAM>((float *)q.y + i0 * q.ldy + j0, q.ldy, M - i0, N - j0, false, lane, value);
     else
-        store_result16<T, T, OUT>((uint16_t *)q.y + i0 * q.ldy + j0, q.ldy, M - i0, N - j0,
-                                  ((uint64_t)(uintptr_t)q.y | (uint64_t)q.ldy * 2) % 4 == 0, lane, value);
+        store_result16<T, T, OUT>((uint16_t *)q.y + i0 * q.ldy + j0, q.ldy, M - i0, N - j0, true, lane, value);
 }
 
 // The slices of a product split along k, summed in their order.  A thread sums four outputs 256 apart.
@@ -273,42 +278,32 @@ __global__ __launch_bounds__(256) void mx4_sum_kernel(const Mx4Params p) {
     }
 }
 
-// ---- few tokens: one pass over b.  A wave has 16 channels, MT x 16 tokens and a share of the groups; the waves' sums meet in LDS, in
-// the order of the waves.  Lane c + 16 g of a fragment has the blocks 2 g and 2 g + 1 of row c of a group, for two matrix instructions,
-// so that the four lanes of a row read its whole line.  U groups are on their way at once.
+// ---- up to 16 tokens: one pass over b.  A wave has 16 channels and a share of the groups; the waves' sums meet in LDS, in the order of the
+// waves.  Lane c + 16 g of a fragment has the blocks 2 g and 2 g + 1 of row c of a group, for two matrix instructions, so that the four
+// lanes of a row read its whole line.  U groups are on their way at once.
 // FUSED: x is converted by every workgroup for itself, into LDS, while the first of b are on their way.
 struct Mx4FewParams {
     Mx4Product q;
     const void *x;
     int64_t ldx;
-    int32_t groups, tiles_n;
+    int32_t groups;
 };
-constexpr int kMx4FusedBytes = 32768;       // of codes
 
-template <int MT, int U, int W, int DT, bool FUSED>
+template <int U, int W, int DT, bool FUSED>
 __global__ __launch_bounds__(64 * W) void gemm_mx4_few_kernel(const Mx4FewParams p) {
-    __shared__ v4f sums[W][MT][64];
-    __shared__ __attribute__((aligned(16))) uint8_t own[FUSED ? kMx4FusedBytes : 16];
-    __shared__ __attribute__((aligned(16))) uint8_t own_scales[FUSED ? kMx4FusedBytes / 16 : 16];
+    __shared__ v4f sums[W][64];
+    extern __shared__ __attribute__((aligned(16))) uint8_t own[];            // FUSED: codes of the tokens, and their scales
     const Mx4Product &q = p.q;
     const int t = threadIdx.x, lane = t & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int64_t M = q.a.rows, N = q.b.rows;
-    const int64_t n0 = (int64_t)(blockIdx.x % p.tiles_n) * 16, m0 = (int64_t)(blockIdx.x / p.tiles_n) * 16 * MT;
+    const int M = (int)q.a.rows;
+    const int64_t N = q.b.rows, n0 = (int64_t)blockIdx.x * 16;
     const int64_t nr = n0 + c < N ? n0 + c : N - 1;
     const uint8_t *const b = q.b.codes + nr * 128 + 32 * g, *const bs = q.b.scales + nr * 8 + 2 * g;
     const int64_t b_step = N * 128, bs_step = q.b.scale_rows * 8, a_step = M * 128, as_step = q.a.scale_rows * 8;
-    const uint8_t *a[MT], *as[MT];
-    if constexpr (!FUSED) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int64_t mr = m0 + 16 * i + c < M ? m0 + 16 * i + c : M - 1;
-            a[i] = q.a.codes + mr * 128 + 32 * g;
-            as[i] = q.a.scales + mr * 8 + 2 * g;
-        }
-    }
-    v4i bw[U][2], aw[U][MT][2];
-    int bsw[U], asw[U][MT];
+    const uint8_t *const a = q.a.codes + (c < M ? c : M - 1) * 128 + 32 * g, *const as = q.a.scales + (c < M ? c : M - 1) * 8 + 2 * g;
+    v4i bw[U][2], aw[U][2];
+    int bsw[U], asw[U];
     const auto request = [&](int s0) {                      // groups s0, s0 + W, ...; past the end the last one again
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -317,20 +312,18 @@ __global__ __launch_bounds__(64 * W) void gemm_mx4_few_kernel(const Mx4FewParams
             bw[u][1] = *reinterpret_cast<const v4i *>(b + at * b_step + 16);
             bsw[u] = *reinterpret_cast<const uint16_t *>(bs + at * bs_step);
             if constexpr (!FUSED) {
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    aw[u][i][0] = *reinterpret_cast<const v4i *>(a[i] + at * a_step);
-                    aw[u][i][1] = *reinterpret_cast<const v4i *>(a[i] + at * a_step + 16);
-                    asw[u][i] = *reinterpret_cast<const uint16_t *>(as[i] + at * as_step);
-                }
+                aw[u][0] = *reinterpret_cast<const v4i *>(a + at * a_step);
+                aw[u][1] = *reinterpret_cast<const v4i *>(a + at * a_step + 16);
+                asw[u] = *reinterpret_cast<const uint16_t *>(as + at * as_step);
             }
         }
     };
     request(wave);
     const int row_bytes = p.groups * 128;
+    uint8_t *const own_scales = own + M * row_bytes;
     if constexpr (FUSED) {
         const int64_t K = q.b.kdim;
-        for (int m = 0; m < (int)M; ++m) {
+        for (int m = 0; m < M; ++m) {
             for (int64_t k = 8 * t; k < p.groups * 256; k += 512 * W) {
                 float x[8];
                 const int64_t left = K - k;
@@ -342,77 +335,86 @@ __global__ __launch_bounds__(64 * W) void gemm_mx4_few_kernel(const Mx4FewParams
         }
         __syncthreads();
     }
-    v4f acc[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) acc[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int s0 = wave; s0 < p.groups; s0 += W * U) {
         if (s0 != wave) request(s0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int s = s0 + u * W;
             if (s < p.groups) {
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    if constexpr (FUSED) {
-                        const int at = (c < M ? c : 0) * row_bytes + s * 128 + 32 * g;
-                        aw[u][i][0] = *reinterpret_cast<const v4i *>(own + at);
-                        aw[u][i][1] = *reinterpret_cast<const v4i *>(own + at + 16);
-                        asw[u][i] = *reinterpret_cast<const uint16_t *>(own_scales + at / 16);
-                    }
-                    acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(four_bit(bw[u][0]), four_bit(aw[u][i][0]), acc[i], 4, 4, 0, bsw[u], 0,
-                                                                              asw[u][i]);
-                    acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(four_bit(bw[u][1]), four_bit(aw[u][i][1]), acc[i], 4, 4, 1, bsw[u], 1,
-                                                                              asw[u][i]);
+                if constexpr (FUSED) {
+                    const int at = (c < M ? c : 0) * row_bytes + s * 128 + 32 * g;
+                    aw[u][0] = *reinterpret_cast<const v4i *>(own + at);
+                    aw[u][1] = *reinterpret_cast<const v4i *>(own + at + 16);
+                    asw[u] = *reinterpret_cast<const uint16_t *>(own_scales + at / 16);
                 }
+                acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(four_bit(bw[u][0]), four_bit(aw[u][0]), acc, 4, 4, 0, bsw[u], 0, asw[u]);
+                acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(four_bit(bw[u][1]), four_bit(aw[u][1]), acc, 4, 4, 1, bsw[u], 1, asw[u]);
             }
         }
     }
-#pragma unroll
-    for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+    sums[wave][lane] = acc;
     __syncthreads();
-    // lane: token c, channels 4 g + v; wave w finishes the token tiles w, w + W, ...
-    for (int i = wave; i < MT; i += W) {
-        v4f all = sums[0][i][lane];
+    if (wave > 0 || c >= M) return;
+    // lane: token c, channels 4 g + v
+    acc = sums[0][lane];
 #pragma unroll
-        for (int w = 1; w < W; ++w) all += sums[w][i][lane];
-        const int64_t m = m0 + 16 * i + c;
-        if (m >= M) continue;
+    for (int w = 1; w < W; ++w) acc += sums[w][lane];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int64_t n = n0 + 4 * g + v;
-            if (n < N) store_float<DT>(q.y, m * q.ldy + n, q.bias ? all[v] + q.bias[n] : all[v]);
-        }
+    for (int v = 0; v < 4; ++v) {
+        const int64_t n = n0 + 4 * g + v;
+        if (n < N) store_float<DT>(q.y, c * q.ldy + n, q.bias ? acc[v] + q.bias[n] : acc[v]);
     }
 }
 
-template <int MT, int U, int W, int DT, bool FUSED>
+template <int U, int W, int DT, bool FUSED>
 int launch_few(Mx4FewParams p, hipStream_t s) {
     p.groups = (int32_t)p.q.b.groups;
-    p.tiles_n = (int32_t)ceil_div(p.q.b.rows, 16);
-    const int64_t wgs = p.tiles_n * ceil_div(p.q.a.rows, 16 * MT);
-    if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
-    hipLaunchKernelGGL((gemm_mx4_few_kernel<MT, U, W, DT, FUSED>), dim3((unsigned)wgs), dim3(64 * W), 0, s, p);
+    const size_t own = FUSED ? (size_t)p.q.a.rows * (size_t)p.groups * 136 : 0;
+    hipLaunchKernelGGL((gemm_mx4_few_kernel<U, W, DT, FUSED>), dim3((unsigned)ceil_div(p.q.b.rows, 16)), dim3(64 * W), own, s, p);
     return launch_status();
 }
 template <int DT>
 int launch_few_of(const Mx4FewParams &p, hipStream_t s) {
-    if (p.q.a.rows > 16) return launch_few<2, 1, 16, DT, false>(p, s);
-    return launch_few<1, 4, 8, DT, false>(p, s);
+    return launch_few<2, 8, DT, false>(p, s);
 }
 template <int DT>
 int launch_fused_of(const Mx4FewParams &p, hipStream_t s) {
-    return launch_few<1, 2, 16, DT, true>(p, s);
+    return p.q.b.groups >= 32 && p.q.b.rows <= 8192 ? launch_few<1, 16, DT, true>(p, s) : launch_few<1, 8, DT, true>(p, s);
 }
 
+// Tile, ring and split of a product: the smallest estimate in us.  `load` workgroups share a compute unit (tiles of 256 x 256 have one to
+// themselves and go in rounds); a launch costs `base`, a workgroup `start`, a group `step` where all units are busy and `lone` more that
+// it takes alone; y costs `out` a Mi output, the slices of a split product `out` for every one written and read.  Fitted to 140 shapes of 17 to
+// 8192 rows and contractions of 100 to 60 000: 1.0 % behind the best of the kernels on average, 18 % at the worst (19 x 516 x 55804).
+// us on tiles of 256, 128 and 64: 8192^3 247, 277, 423; 4096^3 38.7, 41.5, 58.4; 2048 x 4096 x 4096 33.1, 23.3, 32.0; 512 x 4096 x 4096 26.9,
+// 11.7, 9.0; 70 x 5003 x 2730 34, 10.9, 7.3.  Tiles of 64 have a ring of two (four workgroups a unit) or of four (two), which is ahead where
+// fewer find a place anyhow: 24 x 16384 x 8192 13.7 against 17, 512 x 4096 x 4096 9.5 against 9.0.
 struct Mx4Plan {
-    int T, splits;
+    int T, ring, splits;
 };
 Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t groups) {
-    const int64_t tiles4 = ceil_div(M, 256) * ceil_div(N, 256), tiles2 = ceil_div(M, 128) * ceil_div(N, 128);
-    if (tiles4 >= 192) return {4, 1};
-    int64_t splits = 1;
-    while (tiles2 * splits * 2 <= 512 && groups / (splits * 2) >= 4 && splits < 16) splits *= 2;
-    return {2, (int)splits};
+    struct Cost {
+        int T, ring;
+        double base, start, step, lone, out;
+    };
+    static const Cost whole[4] = {{4, 2, 7.5, 14.8, 1.12, 0.0, 0.0},
+                                  {2, 2, 7.2, 0.77, 0.44, 0.09, 0.32},
+                                  {1, 2, 4.4, 0.31, 0.22, 0.10, 0.0},
+                                  {1, 4, 4.3, 0.58, 0.185, 0.056, 0.24}};
+    static const Cost split = {1, 4, 4.9, 2.05, 0.172, 0.118, 0.55};
+    const double outputs = (double)M * (double)N * 1e-6;
+    Mx4Plan best = {1, 4, 1};
+    double least = 0.0;
+    const auto consider = [&](const Cost &c, int64_t splits) {
+        const double wgs = (double)(ceil_div(M, 64 * c.T) * ceil_div(N, 64 * c.T) * splits), g = (double)ceil_div(groups, splits);
+        const double load = c.T == 4 ? ceil(wgs / 256.0) : wgs > 256.0 ? wgs / 256.0 : 1.0, busy = wgs < 256.0 ? wgs / 256.0 : 1.0;
+        const double us = c.base + load * (c.start + g * c.step) + busy * g * c.lone + (double)(splits > 1 ? splits + 1 : 1) * outputs * c.out;
+        if (least == 0.0 || us < least) least = us, best = {c.T, c.ring, (int)splits};
+    };
+    for (const Cost &c : whole) consider(c, 1);
+    for (int64_t s = 2; s <= 32 && groups / s >= 4 && ceil_div(M, 64) * ceil_div(N, 64) * s <= 600; s *= 2) consider(split, s);
+    return best;
 }
 
 template <int T, int RING, int OUT>
@@ -441,7 +443,9 @@ int launch_planned(Mx4Params p, const Mx4Plan &plan, hipStream_t s) {
     g.C = (float *)p.q.y;
     g.ldc = p.q.ldy;
     const bool stream = stores_stream(&g);
-    const int rc = plan.T == 4 ? launch_tiles<4, 2, OUT>(p, stream, s) : launch_tiles<2, 2, OUT>(p, stream, s);
+    const int rc = plan.T == 4   ? launch_tiles<4, 2, OUT>(p, stream, s)
+                   : plan.T == 2 ? launch_tiles<2, 2, OUT>(p, stream, s)
+                                 : (plan.ring == 2 ? launch_tiles<1, 2, OUT>(p, stream, s) : launch_tiles<1, 4, OUT>(p, stream, s));
     if (rc != HBFP_OK || p.splits == 1) return rc;
     const int64_t wgs = ceil_div(g.M * g.N, 1024);
     if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
@@ -449,23 +453,23 @@ int launch_planned(Mx4Params p, const Mx4Plan &plan, hipStream_t s) {
     return launch_status();
 }
 
-bool few_rows(int64_t M, int64_t, int64_t) { return M <= 16; }
+bool few_rows(int64_t M, int64_t N) { return M <= 16 && N < 12288; }
 
 }  // namespace
 
 size_t gemm_mx4_workspace(int64_t M, int64_t N, int64_t groups) {
-    if (few_rows(M, N, groups)) return 0;
+    if (few_rows(M, N)) return 0;
     const Mx4Plan plan = mx4_plan(M, N, groups);
     return plan.splits > 1 ? (size_t)plan.splits * (size_t)M * (size_t)N * 4 : 0;
 }
 
 int launch_gemm_mx4(const Mx4Product &q, void *workspace, hipStream_t s) {
     const int64_t M = q.a.rows, N = q.b.rows, groups = q.b.groups;
-    if (few_rows(M, N, groups)) {
-        const Mx4FewParams p = {q, nullptr, 0, 0, 0};
+    if (few_rows(M, N)) {
+        const Mx4FewParams p = {q, nullptr, 0, 0};
         return q.dtype == HBFP_F32 ? launch_few_of<HBFP_F32>(p, s) : q.dtype == HBFP_BF16 ? launch_few_of<HBFP_BF16>(p, s) : launch_few_of<HBFP_F16>(p, s);
     }
-    if (ceil_div(M, 128) * ceil_div(N, 128) > 0x7ffffff0) return HBFP_ERR_ARG;
+    if (ceil_div(M, 64) * ceil_div(N, 64) > 0x7ffffff0) return HBFP_ERR_ARG;
     const Mx4Plan plan = mx4_plan(M, N, groups);
     const Mx4Params p = {q, (float *)workspace, 0, 0, 0, 0, 0};
     return q.dtype == HBFP_F32    ? launch_planned<kWideF32>(p, plan, s)
@@ -473,10 +477,10 @@ int launch_gemm_mx4(const Mx4Product &q, void *workspace, hipStream_t s) {
                                   : launch_planned<kWideF16>(p, plan, s);
 }
 
-bool linear_mx4_fused_ok(int64_t M, int64_t, int64_t groups) { return M <= 2 && M * groups * 128 <= kMx4FusedBytes; }
+bool linear_mx4_fused_ok(int64_t M, int64_t N, int64_t groups) { return M * (groups > 16 ? groups : 16) <= (N <= 8192 ? 128 : 64); }
 
 int launch_linear_mx4_fused(const Mx4Product &q, const void *x, int64_t ldx, hipStream_t s) {
-    const Mx4FewParams p = {q, x, ldx, 0, 0};
+    const Mx4FewParams p = {q, x, ldx, 0};
     return q.dtype == HBFP_F32 ? launch_fused_of<HBFP_F32>(p, s) : q.dtype == HBFP_BF16 ? launch_fused_of<HBFP_BF16>(p, s) : launch_fused_of<HBFP_F16>(p, s);
 }
 

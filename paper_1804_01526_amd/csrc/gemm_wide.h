@@ -73,10 +73,11 @@ __device__ __forceinline__ uint16_t half_bits(float x) {
 }
 
 // store_result for 16-bit outputs.  Neighbouring lanes hold neighbouring columns of the same rows: of two rows an even lane
-// takes both columns of the first and an odd lane those of the second, so that a lane stores 32 bits (pair: the rows' addresses
-// allow it).
+// takes both columns of the first and an odd lane those of the second, so that a lane stores 32 bits, at addresses that need to be
+// even only (pair; without it one by one).
 template <int TI, int TJ, int OUT, class V>
 __device__ __forceinline__ void store_result16(uint16_t *dst, int64_t ld, int64_t rows, int64_t cols, bool pair, int lane, const V &value) {
+    typedef uint32_t two_at __attribute__((aligned(2)));
     const int lh = lane >> 5, l32 = lane & 31;
     if (rows <= 0 || cols <= 0) return;
     if (rows >= 32 * TI && cols >= 32 * TJ && pair) {
@@ -91,7 +92,7 @@ __device__ __forceinline__ void store_result16(uint16_t *dst, int64_t ld, int64_
                     const uint32_t a = half_bits<OUT>(value(i, j, v)), b = half_bits<OUT>(value(i, j, v + 1));
                     const uint32_t own = odd ? b : a, give = odd ? a : b;
                     const uint32_t got = (uint32_t)__builtin_amdgcn_mov_dpp((int)give, 0xB1, 0xF, 0xF, true);     // lanes 1, 0, 3, 2
-                    *reinterpret_cast<uint32_t *>(p + 32 * j) = odd ? got | own << 16 : own | got << 16;
+                    *reinterpret_cast<two_at *>(p + 32 * j) = odd ? got | own << 16 : own | got << 16;
                 }
                 p += (v & 3) == 2 ? 6 * ld : 2 * ld;
             }
