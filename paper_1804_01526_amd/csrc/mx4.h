@@ -87,6 +87,22 @@ __device__ __forceinline__ uint32_t mx4_code_sr(float x, uint32_t byte, uint32_t
     return code | ((__float_as_uint(x) >> 28) & 8u);
 }
 
+// a word of eight codes -> the values, or pairs of bf16: exact, subnormal results included; the conversion reads the exponent field of its scale
+// alone (0: 2^-127, 255: NaN)
+__device__ __forceinline__ void mx4_values8(uint32_t w, uint32_t byte, float *x) {
+    const float unit = __uint_as_float(byte << 23);
+    const v2f a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 1);
+    const v2f c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 3);
+    x[0] = a[0], x[1] = a[1], x[2] = b[0], x[3] = b[1], x[4] = c[0], x[5] = c[1], x[6] = d[0], x[7] = d[1];
+}
+__device__ __forceinline__ v4u mx4_bf16_8(uint32_t w, uint32_t byte) {
+    const float unit = __uint_as_float(byte << 23);
+    return v4u{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 0)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 1)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 2)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 3))};
+}
+
 // largest magnitude of eight values, as bits (a NaN is larger than everything)
 __device__ __forceinline__ uint32_t mx4_largest8(const float *x) {
     uint32_t amax = 0;

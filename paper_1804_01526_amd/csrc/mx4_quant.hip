@@ -158,26 +158,33 @@ int launch_quant(QuantMx4Params p, bool along, bool down, hipStream_t s) {
     return launch_status();
 }
 
-// ---- back: a thread has a word of eight codes
+// ---- back.  A workgroup has 32 rows of one group; a thread a word of eight codes in four of them, all loads first.
 template <int DT>
-__global__ __launch_bounds__(256) void read_mx4_kernel(const Mx4View t, void *dst, int64_t ld, uint32_t words) {
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t r = e / words;
-    const int64_t k = 8 * (e - r * words);
-    if (r >= t.rows) return;
-    const uint32_t w = *reinterpret_cast<const uint32_t *>(t.codes + ((k >> 8) * t.rows + r) * 128 + ((k & 255) >> 1));
-    const int byte = t.scales[((k >> 8) * t.scale_rows + r) * 8 + ((k & 255) >> 5)];
-    float x[8];
+__global__ __launch_bounds__(256) void read_mx4_kernel(const Mx4View t, void *dst, int64_t ld) {
+    const int64_t group = blockIdx.x % (uint32_t)t.groups, r0 = (int64_t)(blockIdx.x / (uint32_t)t.groups) * 32 + threadIdx.x / 32;
+    const int at = threadIdx.x % 32;
+    const int64_t k = group * 256 + 8 * at, left = t.kdim - k;
+    if (left <= 0) return;
+    uint32_t w[4], byte[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t c = (w >> (4 * i)) & 7u;
-        const float half = (float)((0xC8643210u >> (4 * c)) & 15u);             // the magnitude in halves: 0 1 2 3 4 6 8 12
-        const float v = byte == 255 ? __builtin_nanf("") : __builtin_amdgcn_ldexpf(half, byte - 128);
-        x[i] = (w >> (4 * i)) & 8u ? -v : v;
+    for (int i = 0; i < 4; ++i) {
+        const int64_t r = r0 + 8 * i < t.rows ? r0 + 8 * i : t.rows - 1;
+        w[i] = reinterpret_cast<const uint32_t *>(t.codes + (group * t.rows + r) * 128)[at];
+        byte[i] = t.scales[(group * t.scale_rows + r) * 8 + at / 4];
     }
-    const int64_t left = t.kdim - k;
-    store4<DT>(dst, r * ld + k, left < 4 ? (int)left : 4, x);
-    store4<DT>(dst, r * ld + k + 4, left < 8 ? (int)left - 4 : 4, x + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t r = r0 + 8 * i;
+        if (r >= t.rows) return;
+        if (DT == HBFP_BF16 && left >= 8) {
+            *reinterpret_cast<v4u_at *>(reinterpret_cast<uint16_t *>(dst) + r * ld + k) = mx4_bf16_8(w[i], byte[i]);
+            continue;
+        }
+        float x[8];
+        mx4_values8(w[i], byte[i], x);
+        store4<DT>(dst, r * ld + k, left < 4 ? (int)left : 4, x);
+        store4<DT>(dst, r * ld + k + 4, left < 8 ? (int)left - 4 : 4, x + 4);
+    }
 }
 
 template <int DT>
@@ -198,10 +205,10 @@ int launch_quant_mx4(const void *src, int dtype, int64_t rows, int64_t cols, int
 }
 
 int launch_read_mx4(const Mx4View &t, int dtype, void *dst, int64_t ld, hipStream_t s) {
-    const int64_t words = ceil_div(t.kdim, 8), wgs = ceil_div(words * t.rows, 256);
+    const int64_t wgs = t.groups * ceil_div(t.rows, 32);
     if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
-    if (dtype == HBFP_F32) hipLaunchKernelGGL(read_mx4_kernel<HBFP_F32>, dim3((unsigned)wgs), dim3(256), 0, s, t, dst, ld, (uint32_t)words);
-    else hipLaunchKernelGGL(read_mx4_kernel<HBFP_BF16>, dim3((unsigned)wgs), dim3(256), 0, s, t, dst, ld, (uint32_t)words);
+    if (dtype == HBFP_F32) hipLaunchKernelGGL(read_mx4_kernel<HBFP_F32>, dim3((unsigned)wgs), dim3(256), 0, s, t, dst, ld);
+    else hipLaunchKernelGGL(read_mx4_kernel<HBFP_BF16>, dim3((unsigned)wgs), dim3(256), 0, s, t, dst, ld);
     return launch_status();
 }
 

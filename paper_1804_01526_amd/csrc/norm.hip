@@ -102,13 +102,7 @@ __device__ __forceinline__ void put_mx4(const NormArgs &a, int64_t row, int64_t 
     if (lane % 4 == 0) a.mx4.scales[(group * a.mx4.scale_rows + row) * 8 + ((c & 255) >> 5)] = (uint8_t)byte;
     if (!a.n.values) return;
     float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t k = (w >> (4 * i)) & 7u;
-        const float half = (float)((0xC8643210u >> (4 * k)) & 15u);             // the magnitude in halves
-        const float m = byte == 255u ? __builtin_nanf("") : __builtin_amdgcn_ldexpf(half, (int)byte - 128);
-        v[i] = (w >> (4 * i)) & 8u ? -m : m;
-    }
+    mx4_values8(w, byte, v);
     store8<DT>(a.n.values, row * a.n.ld_values + c, left, v);
 }
 
