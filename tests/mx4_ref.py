@@ -4,23 +4,23 @@ import numpy as np
 MAGNITUDES = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 
 
-def words(rows, cols, seed):
-    """The random word of every element of a matrix, as the public header defines it."""
-    mask = (1 << 32) - 1
-    out = np.zeros((rows, cols), dtype=np.uint64)
-    idx = np.arange(rows * cols, dtype=np.uint64).reshape(rows, cols)
-    lo, hi = idx & np.uint64(mask), idx >> np.uint64(32)
-    x = lo ^ np.uint64(seed & mask)
+def words_at(idx, seed):
+    """The random words of the elements at positions idx of a matrix, as the public header defines them."""
+    mask = np.uint64((1 << 32) - 1)
+    idx = np.asarray(idx, dtype=np.uint64)
+    x = (idx & mask) ^ np.uint64(seed & 0xFFFFFFFF)
     for shift, left in ((13, True), (17, False), (5, True)):
-        x = (x ^ ((x << np.uint64(shift)) if left else (x >> np.uint64(shift)))) & np.uint64(mask)
-    x = (x + (hi ^ np.uint64(seed >> 32))) & np.uint64(mask)
+        x = (x ^ ((x << np.uint64(shift)) if left else (x >> np.uint64(shift)))) & mask
+    x = (x + ((idx >> np.uint64(32)) ^ np.uint64(seed >> 32))) & mask
     x ^= x >> np.uint64(16)
-    x = (x * np.uint64(0x85EBCA6B)) & np.uint64(mask)
+    x = (x * np.uint64(0x85EBCA6B)) & mask
     x ^= x >> np.uint64(13)
-    x = (x * np.uint64(0xC2B2AE35)) & np.uint64(mask)
-    x ^= x >> np.uint64(16)
-    out[:] = x
-    return out
+    x = (x * np.uint64(0xC2B2AE35)) & mask
+    return x ^ (x >> np.uint64(16))
+
+
+def words(rows, cols, seed):
+    return words_at(np.arange(rows * cols, dtype=np.uint64).reshape(rows, cols), seed)
 
 
 def quant(x, h=None):
