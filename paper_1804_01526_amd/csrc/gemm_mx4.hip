@@ -374,6 +374,9 @@ int launch_few(Mx4FewParams p, hipStream_t s) {
     hipLaunchKernelGGL((gemm_mx4_few_kernel<U, W, DT, FUSED>), dim3((unsigned)ceil_div(p.q.b.rows, 16)), dim3(64 * W), own, s, p);
     return launch_status();
 }
+// Waves of a workgroup and groups on their way (W x U).  us with 4 x 4, 8 x 1, 8 x 2: 16 x 4096 x 4096 4.3 all, 1 x 4096 x 4096 3.5, 3.7, 3.6;
+// converting inside, with 8 x 1, 8 x 2, 16 x 1: 1 x 4096 x 4096 3.9, 3.8, 3.9, 1 x 16384 x 4096 7.4, 7.8, 8.7, but 1 x 8192 x 8192 8.5, 8.1, 7.4, 4 x 8192 x
+// 8192 11.4, 11.4, 10.5
 template <int DT>
 int launch_few_of(const Mx4FewParams &p, hipStream_t s) {
     return launch_few<2, 8, DT, false>(p, s);
@@ -453,19 +456,22 @@ int launch_planned(Mx4Params p, const Mx4Plan &plan, hipStream_t s) {
     return launch_status();
 }
 
-bool few_rows(int64_t M, int64_t N) { return M <= 16 && N < 12288; }
+// Up to 16 tokens are one pass over b, on its own kernel or on tiles of 64 channels.  us on the one and the other: 16 x 4096 x 4096 4.3 and 6.4,
+// 16 x 8192 x 1024 3.3 and 4.4, 1 x 1024 x 16384 7.2 and 14; but where there are tiles enough, 16 x 16384 x 8192 18.6 and 13.6, 16 x 12288 x 4096
+// 8.2 and 6.9, and where the contraction is long enough to be split, 16 x 512 x 16384 10.5 and 8.2, 4 x 2048 x 30000 16.4 and 10.7.
+bool few_rows(int64_t M, int64_t N, int64_t groups) { return M <= 16 && N < 12288 && groups < 64; }
 
 }  // namespace
 
 size_t gemm_mx4_workspace(int64_t M, int64_t N, int64_t groups) {
-    if (few_rows(M, N)) return 0;
+    if (few_rows(M, N, groups)) return 0;
     const Mx4Plan plan = mx4_plan(M, N, groups);
     return plan.splits > 1 ? (size_t)plan.splits * (size_t)M * (size_t)N * 4 : 0;
 }
 
 int launch_gemm_mx4(const Mx4Product &q, void *workspace, hipStream_t s) {
     const int64_t M = q.a.rows, N = q.b.rows, groups = q.b.groups;
-    if (few_rows(M, N)) {
+    if (few_rows(M, N, groups)) {
         const Mx4FewParams p = {q, nullptr, 0, 0};
         return q.dtype == HBFP_F32 ? launch_few_of<HBFP_F32>(p, s) : q.dtype == HBFP_BF16 ? launch_few_of<HBFP_BF16>(p, s) : launch_few_of<HBFP_F16>(p, s);
     }
@@ -477,6 +483,9 @@ int launch_gemm_mx4(const Mx4Product &q, void *workspace, hipStream_t s) {
                                   : launch_planned<kWideF16>(p, plan, s);
 }
 
+// What converting x in every workgroup costs grows with the tokens and the workgroups.  us fused and in two launches (each of which also costs
+// the host 4): 1 x 4096 x 4096 3.9 and 6.3, 4 x 4096 x 4096 5.0 and 6.5, 8 x 4096 x 4096 6.5 and 6.7, 16 x 4096 x 4096 9.0 and 7.0; 1 x 16384 x 8192
+// 13.4 and 15.8, 2 x 16384 x 8192 15.0 and 15.8, 4 x 16384 x 8192 17.2 and 15.9
 bool linear_mx4_fused_ok(int64_t M, int64_t N, int64_t groups) { return M * (groups > 16 ? groups : 16) <= (N <= 8192 ? 128 : 64); }
 
 int launch_linear_mx4_fused(const Mx4Product &q, const void *x, int64_t ldx, hipStream_t s) {

@@ -10,7 +10,7 @@ struct QuantMx4Params {
     int64_t rows, cols, ld;
     uint32_t s0, s1;
     Mx4View along, down;
-    uint32_t tiles_c;            // tiles along the source's columns
+    uint32_t tiles_c, tiles;     // tiles along the source's columns, all tiles
 };
 
 template <int ROUND>
@@ -68,7 +68,12 @@ template <int DT, int ROUND, bool ALONG>
 __global__ __launch_bounds__(256, ALONG && ROUND == HBFP_STOCHASTIC ? 3 : 4) void quant_mx4_down_kernel(const QuantMx4Params p) {
     __shared__ __attribute__((aligned(16))) uint32_t words[128][20];     // 16 of column 8 a + b in row 16 b + a: a wave's writes cover all banks
     const int t = threadIdx.x, lane = t & 63, tr = t / 16;
-    const int64_t c0 = (int64_t)(blockIdx.x % p.tiles_c) * 128, r0 = (int64_t)(blockIdx.x / p.tiles_c) * 128;
+    // workgroups are dealt to the 8 XCDs in turn: each gets a run of tiles, two rows of them side by side, so that the halves of a line of codes
+    // of either operand meet in one L2
+    const uint32_t tile = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    if (tile >= p.tiles) return;
+    const uint32_t band = tile / (2 * p.tiles_c), in_band = tile - band * 2 * p.tiles_c;
+    const int64_t c0 = (int64_t)(in_band >> 1) * 128, r0 = ((int64_t)band * 2 + (in_band & 1)) * 128;
     const int64_t c = c0 + 8 * (t % 16), r = r0 + 8 * tr, left = p.cols - c;
     float x[8][8];
 #pragma unroll
@@ -132,7 +137,7 @@ __global__ __launch_bounds__(256, ALONG && ROUND == HBFP_STOCHASTIC ? 3 : 4) voi
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int col = 64 * i + t / 4;
+        const int col = 8 * (lane / 4) + t / 64 + 4 * i;     // (columns 8 apart: neighbouring rows of words, every bank once)
         if (c0 + col < p.cols)
             *reinterpret_cast<v4u *>(p.down.codes + (group * p.cols + c0 + col) * 128 + ((r0 & 255) >> 1) + 16 * (t % 4)) =
                 *reinterpret_cast<const v4u *>(&words[16 * (col % 8) + col / 8][4 * (t % 4)]);
@@ -151,10 +156,11 @@ int launch_quant(QuantMx4Params p, bool along, bool down, hipStream_t s) {
     // whole groups of whichever operands are wanted: what is past the source is stored as zeros
     const int64_t tiles_c = along ? 2 * p.along.groups : ceil_div(p.cols, 128), tiles_r = 2 * p.down.groups;
     const int64_t wgs = tiles_c * tiles_r;
-    if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
+    if (wgs > 0x7ffffff0 || tiles_c > 0x3fffffff) return HBFP_ERR_ARG;
     p.tiles_c = (uint32_t)tiles_c;
+    p.tiles = (uint32_t)wgs;
     void (*const kernel)(QuantMx4Params) = along ? &quant_mx4_down_kernel<DT, ROUND, true> : &quant_mx4_down_kernel<DT, ROUND, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)round_up(wgs, 8)), dim3(256), 0, s, p);
     return launch_status();
 }
 
@@ -196,7 +202,7 @@ int launch_quant_of(const QuantMx4Params &p, int rounding, bool along, bool down
 
 int launch_quant_mx4(const void *src, int dtype, int64_t rows, int64_t cols, int64_t ld, int rounding, uint64_t seed, const Mx4View *along,
                      const Mx4View *down, hipStream_t s) {
-    QuantMx4Params p = {src, rows, cols, ld, (uint32_t)seed, (uint32_t)(seed >> 32), {}, {}, 0};
+    QuantMx4Params p = {src, rows, cols, ld, (uint32_t)seed, (uint32_t)(seed >> 32), {}, {}, 0, 0};
     if (along) p.along = *along;
     if (down) p.down = *down;
     return dtype == HBFP_F32    ? launch_quant_of<HBFP_F32>(p, rounding, along, down, s)

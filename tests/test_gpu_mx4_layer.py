@@ -101,7 +101,9 @@ DT = {F32: 0, BF16: 1, F16: 2}
 @pytest.mark.parametrize("m,n,k,dtype,names", [
     (3, 700, 900, F32, ["gemm_mx4_few_kernel<2, 8, {}, false>"]),
     (16, 500, 5000, BF16, ["gemm_mx4_few_kernel<2, 8, {}, false>"]),
-    (16, 300, 70000, F16, ["gemm_mx4_few_kernel<2, 8, {}, false>"]),
+    (16, 300, 16128, F16, ["gemm_mx4_few_kernel<2, 8, {}, false>"]),
+    (16, 300, 16129, F16, ["gemm_mx4_kernel<1, 4, 3, false>", "mx4_sum_kernel<3>"]),
+    (1, 300, 70000, BF16, ["gemm_mx4_kernel<1, 4, 2, false>", "mx4_sum_kernel<2>"]),
     (5, 12300, 600, BF16, ["gemm_mx4_kernel<1, 4, 2, false>"]),
     (40, 2000, 1500, BF16, ["gemm_mx4_kernel<1, 4, 2, false>"]),
     (130, 90, 1100, F32, ["gemm_mx4_kernel<1, 4, 1, true>"]),
@@ -136,7 +138,7 @@ def test_kernels_of_the_product(hb, m, n, k, dtype, names):
     (1, 40, 32700, ["gemm_mx4_few_kernel<1, 16, {}, true>"]),
     (2, 12300, 8100, ["gemm_mx4_few_kernel<1, 8, {}, true>"]),
     (9, 1000, 4000, ["quant_mx4_along_kernel<{}, 0>", "gemm_mx4_few_kernel<2, 8, {}, false>"]),
-    (1, 40, 32800, ["quant_mx4_along_kernel<{}, 0>", "gemm_mx4_few_kernel<2, 8, {}, false>"]),
+    (4, 40, 8200, ["quant_mx4_along_kernel<{}, 0>", "gemm_mx4_few_kernel<2, 8, {}, false>"]),
 ])
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_kernels_of_the_linear_layer(hb, m, n, k, names, dtype):
