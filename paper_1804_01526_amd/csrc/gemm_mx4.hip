@@ -389,9 +389,9 @@ int launch_fused_of(const Mx4FewParams &p, hipStream_t s) {
 // Tile, ring and split of a product: the smallest estimate in us.  `load` workgroups share a compute unit (tiles of 256 x 256 have one to
 // themselves and go in rounds); a launch costs `base`, a workgroup `start`, a group `step` where all units are busy and `lone` more that
 // it takes alone; y costs `out` a Mi output, the slices of a split product `out` for every one written and read.  Fitted to 140 shapes of 17 to
-// 8192 rows and contractions of 100 to 60 000: 1.0 % behind the best of the kernels on average, 18 % at the worst (19 x 516 x 55804).
-// us on tiles of 256, 128 and 64: 8192^3 247, 277, 423; 4096^3 38.7, 41.5, 58.4; 2048 x 4096 x 4096 33.1, 23.3, 32.0; 512 x 4096 x 4096 26.9,
-// 11.7, 9.0; 70 x 5003 x 2730 34, 10.9, 7.3.  Tiles of 64 have a ring of two (four workgroups a unit) or of four (two), which is ahead where
+// 8192 rows and contractions of 100 to 60 000: 0.9 % behind the best of the kernels on average, 18 % at the worst (19 x 516 x 55804).
+// us on tiles of 256, 128 and 64: 8192^3 248, 275, 423; 4096^3 38.4, 41.0, 58.4; 2048 x 4096 x 4096 33.1, 23.3, 32.0; 3000 x 6000 x 3000 57, 39, 50;
+// 512 x 4096 x 4096 26.9, 11.7, 9.0; 70 x 5003 x 2730 34, 10.9, 7.3.  Tiles of 64 have a ring of two (four workgroups a unit) or of four (two), which is ahead where
 // fewer find a place anyhow: 24 x 16384 x 8192 13.7 against 17, 512 x 4096 x 4096 9.5 against 9.0.
 struct Mx4Plan {
     int T, ring, splits;
@@ -401,11 +401,11 @@ Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t groups) {
         int T, ring;
         double base, start, step, lone, out;
     };
-    static const Cost whole[4] = {{4, 2, 7.5, 14.8, 1.12, 0.0, 0.0},
-                                  {2, 2, 7.2, 0.77, 0.44, 0.09, 0.32},
-                                  {1, 2, 4.4, 0.31, 0.22, 0.10, 0.0},
-                                  {1, 4, 4.3, 0.58, 0.185, 0.056, 0.24}};
-    static const Cost split = {1, 4, 4.9, 2.05, 0.172, 0.118, 0.55};
+    static const Cost whole[4] = {{4, 2, 5.4, 10.2, 1.29, 0.0, 0.0},
+                                  {2, 2, 5.3, 0.0, 0.45, 0.14, 0.40},
+                                  {1, 2, 3.3, 0.35, 0.22, 0.10, 0.0},
+                                  {1, 4, 3.2, 0.51, 0.19, 0.06, 0.30}};
+    static const Cost split = {1, 4, 4.9, 2.0, 0.17, 0.11, 0.63};
     const double outputs = (double)M * (double)N * 1e-6;
     Mx4Plan best = {1, 4, 1};
     double least = 0.0;

@@ -98,6 +98,28 @@ __device__ __forceinline__ void store_result16(uint16_t *dst, int64_t ld, int64_
             }
         return;
     }
+    if (pair) {                                             // at the edges of y
+        const bool odd = lane & 1;
+        const int r_end = (int)(rows < 32 * TI ? rows : 32 * TI) - 4 * lh - odd, c_end = (int)(cols < 32 * TJ ? cols : 32 * TJ) - (l32 & ~1);
+        uint16_t *p = dst + (4 * lh + odd) * ld + (l32 & ~1);
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int v = 0; v < 16; v += 2) {
+#pragma unroll
+                for (int j = 0; j < TJ; ++j) {
+                    const uint32_t a = half_bits<OUT>(value(i, j, v)), b = half_bits<OUT>(value(i, j, v + 1));
+                    const uint32_t own = odd ? b : a, give = odd ? a : b;
+                    const uint32_t got = (uint32_t)__builtin_amdgcn_mov_dpp((int)give, 0xB1, 0xF, 0xF, true);
+                    const uint32_t two = odd ? got | own << 16 : own | got << 16;
+                    if (32 * i + 8 * (v >> 2) + (v & 3) >= r_end) continue;
+                    if (32 * j + 1 < c_end) *reinterpret_cast<two_at *>(p + 32 * j) = two;
+                    else if (32 * j < c_end) p[32 * j] = (uint16_t)two;
+                }
+                p += (v & 3) == 2 ? 6 * ld : 2 * ld;
+            }
+        return;
+    }
     const int r_end = (int)(rows < 32 * TI ? rows : 32 * TI) - 4 * lh, c_end = (int)(cols < 32 * TJ ? cols : 32 * TJ) - l32;
     uint16_t *p = dst + 4 * lh * ld + l32;
 #pragma unroll
