@@ -53,7 +53,7 @@ bool overlap(const Span &x, const Span &y) {
 }
 
 int check_matrix(const void *p, int dtype, int64_t rows, int64_t cols, int64_t ld) {
-    if (!p || rows <= 0 || cols <= 0 || rows > 0x7fffffff || cols > 0x7fffff00 || ld < cols || ld > ((int64_t)1 << 40)) return HBFP_ERR_ARG;
+    if (!p || rows <= 0 || cols <= 0 || rows > 0x7fffffff || cols > 0x7fffff00 || ld < cols || ld > ((int64_t)1 << 60) / rows) return HBFP_ERR_ARG;
     if (!known_type(dtype)) return HBFP_ERR_FORMAT;
     return (uintptr_t)p & (size_of(dtype) - 1) ? HBFP_ERR_ARG : HBFP_OK;
 }

@@ -65,23 +65,23 @@ def test_product_refusals():
     n = ctypes.c_size_t(0)
     assert L.hbfp_gemm_mx4_workspace(0, 1, 1, ref(n)) == hbfp.ERR_ARG and L.hbfp_gemm_mx4_workspace(1, 1, 1, None) == hbfp.ERR_ARG
     assert L.hbfp_linear_mx4_workspace(1, 1 << 31, 1, ref(n)) == hbfp.ERR_ARG
-    a, b = _op(40, 4000), _op(24, 4000, P + 2 * FAR)
-    need = hbfp.gemm_mx4_workspace(40, 24, 4000)
+    a, b = _op(40, 40000), _op(24, 40000, P + 2 * FAR)
+    need = hbfp.gemm_mx4_workspace(40, 24, 40000)
     assert need % 256 == 0 and need > 0
 
     def gemm(a=a, b=b, bias=None, y=P + FAR, dtype=1, ldy=24, ws=P, size=need):
         return L.hbfp_gemm_mx4(ref(a) if a else None, ref(b) if b else None, bias, y, dtype, ldy, ws, size, None)
 
-    assert gemm(a=None) == hbfp.ERR_ARG and gemm(b=None) == hbfp.ERR_ARG and gemm(b=_op(24, 3999, P + 2 * FAR)) == hbfp.ERR_LAYOUT
+    assert gemm(a=None) == hbfp.ERR_ARG and gemm(b=None) == hbfp.ERR_ARG and gemm(b=_op(24, 39999, P + 2 * FAR)) == hbfp.ERR_LAYOUT
     assert gemm(y=None) == hbfp.ERR_ARG and gemm(ldy=23) == hbfp.ERR_ARG and gemm(dtype=4) == hbfp.ERR_FORMAT and gemm(y=P + FAR + 1) == hbfp.ERR_ARG
     assert gemm(bias=P + 2) == hbfp.ERR_ARG and gemm(bias=P + FAR) == hbfp.ERR_ARG and gemm(y=P) == hbfp.ERR_ARG
     assert gemm(ws=None) == hbfp.ERR_WORKSPACE and gemm(size=need - 1) == hbfp.ERR_WORKSPACE and gemm(ws=P + 128) == hbfp.ERR_WORKSPACE
-    need = hbfp.linear_mx4_workspace(40, 24, 4000)
+    need = hbfp.linear_mx4_workspace(40, 24, 40000)
 
-    def linear(x=P + FAR, dtype=1, m=40, ldx=4000, w=b, y=P + 3 * FAR, ldy=24, ws=P, size=need):
+    def linear(x=P + FAR, dtype=1, m=40, ldx=40000, w=b, y=P + 3 * FAR, ldy=24, ws=P, size=need):
         return L.hbfp_linear_mx4(x, dtype, m, ldx, ref(w), None, y, ldy, ws, size, None)
 
-    assert linear(x=None) == hbfp.ERR_ARG and linear(ldx=3999) == hbfp.ERR_ARG and linear(m=0) == hbfp.ERR_ARG and linear(dtype=5) == hbfp.ERR_FORMAT
+    assert linear(x=None) == hbfp.ERR_ARG and linear(ldx=39999) == hbfp.ERR_ARG and linear(m=0) == hbfp.ERR_ARG and linear(dtype=5) == hbfp.ERR_FORMAT
     assert linear(y=None) == hbfp.ERR_ARG and linear(y=P + 2 * FAR) == hbfp.ERR_ARG and linear(size=need - 1) == hbfp.ERR_WORKSPACE
 
 
