@@ -303,7 +303,7 @@ __global__ __launch_bounds__(64 * W) void gemm_mx4_few_kernel(const Mx4FewParams
     const int t = threadIdx.x, lane = t & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int M = (int)q.a.rows;
-    const int64_t N = q.b.rows, n0 = (int64_t)blockIdx.x * 16;
+    const int64_t N = q.b.rows, n0 = (int64_t)workgroup() * 16;
     const int64_t nr = n0 + c < N ? n0 + c : N - 1;
     const uint8_t *const b = q.b.codes + nr * 128 + 32 * g, *const bs = q.b.scales + nr * 8 + 2 * g;
     const int64_t b_step = N * 128, bs_step = q.b.scale_rows * 8, a_step = M * 128, as_step = q.a.scale_rows * 8;
@@ -377,7 +377,7 @@ template <int U, int W, int DT, bool FUSED>
 int launch_few(Mx4FewParams p, hipStream_t s) {
     p.groups = (int32_t)p.q.b.groups;
     const size_t own = FUSED ? (size_t)p.q.a.rows * (size_t)p.groups * 136 : 0;
-    hipLaunchKernelGGL((gemm_mx4_few_kernel<U, W, DT, FUSED>), dim3((unsigned)ceil_div(p.q.b.rows, 16)), dim3(64 * W), own, s, p);
+    hipLaunchKernelGGL((gemm_mx4_few_kernel<U, W, DT, FUSED>), grid_of(ceil_div(p.q.b.rows, 16)), dim3(64 * W), own, s, p);
     return launch_status();
 }
 // Waves of a workgroup and groups on their way (W x U).  us with 4 x 4, 8 x 1, 8 x 2: 16 x 4096 x 4096 4.3 all, 1 x 4096 x 4096 3.5, 3.7, 3.6;
@@ -456,9 +456,7 @@ int launch_planned(Mx4Params p, const Mx4Plan &plan, hipStream_t s) {
                    : plan.T == 2 ? launch_tiles<2, 2, OUT>(p, stream, s)
                                  : (plan.ring == 2 ? launch_tiles<1, 2, OUT>(p, stream, s) : launch_tiles<1, 4, OUT>(p, stream, s));
     if (rc != HBFP_OK || p.splits == 1) return rc;
-    const int64_t wgs = ceil_div(g.M * g.N, 1024);
-    if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
-    hipLaunchKernelGGL(mx4_sum_kernel<OUT>, dim3((unsigned)wgs), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(mx4_sum_kernel<OUT>, dim3((unsigned)ceil_div(g.M * g.N, 1024)), dim3(256), 0, s, p);
     return launch_status();
 }
 
@@ -468,6 +466,12 @@ int launch_planned(Mx4Params p, const Mx4Plan &plan, hipStream_t s) {
 bool few_rows(int64_t M, int64_t N, int64_t groups) { return M <= 16 && N < 12288 && groups < 64; }
 
 }  // namespace
+
+bool gemm_mx4_fits(int64_t M, int64_t N, int64_t groups) {
+    if (one_row(round_up(ceil_div(M, 64) * ceil_div(N, 64), 8), 256) || few_rows(M, N, groups)) return true;
+    const int T = mx4_plan(M, N, groups).T;
+    return one_row(round_up(ceil_div(M, 64 * T) * ceil_div(N, 64 * T), 8), 256);
+}
 
 size_t gemm_mx4_workspace(int64_t M, int64_t N, int64_t groups) {
     if (few_rows(M, N, groups)) return 0;
@@ -481,7 +485,6 @@ int launch_gemm_mx4(const Mx4Product &q, void *workspace, hipStream_t s) {
         const Mx4FewParams p = {q, nullptr, 0, 0};
         return q.dtype == HBFP_F32 ? launch_few_of<HBFP_F32>(p, s) : q.dtype == HBFP_BF16 ? launch_few_of<HBFP_BF16>(p, s) : launch_few_of<HBFP_F16>(p, s);
     }
-    if (ceil_div(M, 64) * ceil_div(N, 64) > 0x7ffffff0) return HBFP_ERR_ARG;
     const Mx4Plan plan = mx4_plan(M, N, groups);
     const Mx4Params p = {q, (float *)workspace, 0, 0, 0, 0, 0};
     return q.dtype == HBFP_F32    ? launch_planned<kWideF32>(p, plan, s)

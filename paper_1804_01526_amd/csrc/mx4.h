@@ -23,6 +23,8 @@ struct Mx4Product {
     int64_t ldy;
     int32_t dtype;
 };
+// whether a launch can hold the product's tiles
+bool gemm_mx4_fits(int64_t M, int64_t N, int64_t groups);
 size_t gemm_mx4_workspace(int64_t M, int64_t N, int64_t groups);
 int launch_gemm_mx4(const Mx4Product &p, void *workspace, hipStream_t s);
 // x converted inside the product: few tokens whose codes fit into LDS; p.a's buffers are not read
@@ -50,6 +52,16 @@ size_t norm_grad_workspace(int64_t rows, int64_t cols);
 int launch_norm_grad(const NormGradArgs &a, hipStream_t s);
 
 namespace {
+
+// One dimension of a launch has fewer than 2^32 threads: more than 2^21 workgroups go in rows of that many, and those behind the last find
+// nothing to do.
+constexpr int kGridBits = 21;
+inline dim3 grid_of(int64_t wgs) {
+    return wgs <= 1 << kGridBits ? dim3((unsigned)wgs) : dim3(1u << kGridBits, (unsigned)ceil_div(wgs, (int64_t)1 << kGridBits));
+}
+__device__ __forceinline__ uint32_t workgroup() { return (blockIdx.y << kGridBits) + blockIdx.x; }
+// launches whose workgroups are counted otherwise have to fit into one row
+inline bool one_row(int64_t wgs, int threads) { return wgs * threads <= 0xffffffffll; }
 
 // the byte of a block from the bit pattern of its largest magnitude: adding what rounds up carries into the exponent field
 template <int ROUND>

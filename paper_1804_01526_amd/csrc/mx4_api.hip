@@ -167,6 +167,7 @@ int hbfp_gemm_mx4(const hbfp_mx4 *a, const hbfp_mx4 *b, const float *bias, void 
                         bytes_at(b->scales, b->scale_bytes), bytes_at(bias, 4 * (uint64_t)b->rows)};
     for (const Span &i : in)
         if (overlap(out, i)) return HBFP_ERR_ARG;
+    if (!gemm_mx4_fits(a->rows, b->rows, a->groups)) return HBFP_ERR_ARG;
     const size_t need = align256(gemm_mx4_workspace(a->rows, b->rows, a->groups));
     if (need && (!workspace || ws_bytes < need || ((uintptr_t)workspace & 255))) return HBFP_ERR_WORKSPACE;
     const Mx4Product p = {view_of(*a), view_of(*b), bias, y, ldy, dtype};
@@ -202,6 +203,7 @@ int hbfp_linear_mx4(const void *x, int dtype, int64_t M, int64_t ldx, const hbfp
         if (overlap(out, matrix(x, dtype, M, K, ldx))) return HBFP_ERR_ARG;
         return launch_linear_mx4_fused(p, x, ldx, (hipStream_t)stream);
     }
+    if (!gemm_mx4_fits(M, N, codes.groups)) return HBFP_ERR_ARG;
     size_t need = 0;
     if ((rc = hbfp_linear_mx4_workspace(M, N, K, &need)) != HBFP_OK) return rc;
     if (!workspace || ws_bytes < need || ((uintptr_t)workspace & 255)) return HBFP_ERR_WORKSPACE;

@@ -48,7 +48,7 @@ __device__ __forceinline__ uint32_t codes8(const float *x, uint32_t byte, int64_
 template <int DT, int ROUND>
 __global__ __launch_bounds__(256) void quant_mx4_along_kernel(const QuantMx4Params p) {
     const int t = threadIdx.x;
-    const int64_t group = blockIdx.x % p.tiles_c, r0 = (int64_t)(blockIdx.x / p.tiles_c) * 32 + t / 32;
+    const int64_t group = workgroup() % p.tiles_c, r0 = (int64_t)(workgroup() / p.tiles_c) * 32 + t / 32;
     const int64_t c = group * 256 + 8 * (t % 32);
     const int64_t left = p.cols - c;
     float x[4][8];
@@ -168,13 +168,13 @@ int launch_quant(QuantMx4Params p, bool along, bool down, hipStream_t s) {
         p.tiles_c = (uint32_t)p.along.groups;
         const int64_t wgs = p.along.groups * ceil_div(p.rows, 32);
         if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
-        hipLaunchKernelGGL((quant_mx4_along_kernel<DT, ROUND>), dim3((unsigned)wgs), dim3(256), 0, s, p);
+        hipLaunchKernelGGL((quant_mx4_along_kernel<DT, ROUND>), grid_of(wgs), dim3(256), 0, s, p);
         return launch_status();
     }
     // whole groups of whichever operands are wanted: what is past the source is stored as zeros
     const int64_t tiles_c = along ? 2 * p.along.groups : ceil_div(p.cols, 128), tiles_r = 2 * p.down.groups;
     const int64_t wgs = tiles_c * tiles_r;
-    if (wgs > 0x7ffffff0 || tiles_c > 0x3fffffff) return HBFP_ERR_ARG;
+    if (!one_row(round_up(wgs, 8), 256)) return HBFP_ERR_ARG;
     p.tiles_c = (uint32_t)tiles_c;
     p.tiles = (uint32_t)wgs;
     void (*const kernel)(QuantMx4Params) = along ? &quant_mx4_down_kernel<DT, ROUND, true> : &quant_mx4_down_kernel<DT, ROUND, false>;
@@ -186,7 +186,7 @@ int launch_quant(QuantMx4Params p, bool along, bool down, hipStream_t s) {
 // 5.6 to 6.4 TB/s.
 template <int DT>
 __global__ __launch_bounds__(256) void read_mx4_kernel(const Mx4View t, void *dst, int64_t ld) {
-    const int64_t group = blockIdx.x % (uint32_t)t.groups, r0 = (int64_t)(blockIdx.x / (uint32_t)t.groups) * 32 + threadIdx.x / 32;
+    const int64_t group = workgroup() % (uint32_t)t.groups, r0 = (int64_t)(workgroup() / (uint32_t)t.groups) * 32 + threadIdx.x / 32;
     const int at = threadIdx.x % 32;
     const int64_t k = group * 256 + 8 * at, left = t.kdim - k;
     if (left <= 0) return;
@@ -232,8 +232,8 @@ int launch_quant_mx4(const void *src, int dtype, int64_t rows, int64_t cols, int
 int launch_read_mx4(const Mx4View &t, int dtype, void *dst, int64_t ld, hipStream_t s) {
     const int64_t wgs = t.groups * ceil_div(t.rows, 32);
     if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
-    if (dtype == HBFP_F32) hipLaunchKernelGGL(read_mx4_kernel<HBFP_F32>, dim3((unsigned)wgs), dim3(256), 0, s, t, dst, ld);
-    else hipLaunchKernelGGL(read_mx4_kernel<HBFP_BF16>, dim3((unsigned)wgs), dim3(256), 0, s, t, dst, ld);
+    if (dtype == HBFP_F32) hipLaunchKernelGGL(read_mx4_kernel<HBFP_F32>, grid_of(wgs), dim3(256), 0, s, t, dst, ld);
+    else hipLaunchKernelGGL(read_mx4_kernel<HBFP_BF16>, grid_of(wgs), dim3(256), 0, s, t, dst, ld);
     return launch_status();
 }
 

@@ -117,7 +117,7 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_kernel(const NormAr
     __shared__ uint32_t meet_top[W];
     const hbfp_norm &n = a.n;
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : threadIdx.x >> 6;
-    const int64_t row = (int64_t)blockIdx.x * kRows + (W == 1 ? threadIdx.x >> 6 : 0);
+    const int64_t row = (int64_t)workgroup() * kRows + (W == 1 ? threadIdx.x >> 6 : 0);
     if (row >= n.rows) return;                               // (a whole wave, and W = 1 has no barrier)
     constexpr int64_t kStep = 512 * W;
     const int64_t c0 = 8 * (64 * wave + lane);
@@ -191,7 +191,7 @@ template <int DT, int FORM, int W, int KEEP, bool LOOP>
 int launch(const NormArgs &a, hipStream_t s) {
     constexpr int kRows = W < 4 ? 4 / W : 1;
     const int64_t wgs = ceil_div(a.n.rows, kRows);
-    hipLaunchKernelGGL((norm_kernel<DT, FORM, W, KEEP, LOOP>), dim3((unsigned)wgs), dim3(W < 4 ? 256 : 64 * W), 0, s, a);
+    hipLaunchKernelGGL((norm_kernel<DT, FORM, W, KEEP, LOOP>), grid_of(wgs), dim3(W < 4 ? 256 : 64 * W), 0, s, a);
     return launch_status();
 }
 // us (bf16, 8-bit rows) on as many waves, with as many times 8 columns a lane: 8192 x 2048 on 4 28.2, on 1 (x 4) 29.9, on 8 40.4; 4096 x 4096 on 4 (x 2) 27.7,
@@ -329,7 +329,8 @@ template <int DT>
 __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const NormGradArgs a) {
     __shared__ float meet[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = blockIdx.x;
+    const int64_t row = workgroup();
+    if (row >= a.rows) return;
     const float r = a.rstd[row];
     const auto load = [&](int64_t c, int left, float *g, float *u, float *w) {
         load8<DT>(a.g, row * a.ldg + c, left, g);
@@ -389,7 +390,7 @@ __global__ __launch_bounds__(32 * kShares) void norm_dweight_sum_kernel(const Gr
     __shared__ float meet[kShares][32];
     const NormGradArgs &a = p.a;
     const int lane = threadIdx.x & 31, share = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    const int64_t c = (int64_t)workgroup() * 32 + lane;
     const int per = (p.wgs + kShares - 1) / kShares, end = (share + 1) * per < p.wgs ? (share + 1) * per : p.wgs;
     float sum = 0.0f;
     if (c < a.cols)
@@ -436,9 +437,9 @@ int launch_grad(const NormGradArgs &a, hipStream_t s) {
     else {
         // (dx may be written over g)
         if (a.dweight) hipLaunchKernelGGL(norm_dweight_kernel<DT>, dim3((unsigned)ceil_div(a.cols, 2048), (unsigned)p.wgs), dim3(256), 0, s, p);
-        hipLaunchKernelGGL(norm_grad_long_kernel<DT>, dim3((unsigned)a.rows), dim3(1024), 0, s, a);
+        hipLaunchKernelGGL(norm_grad_long_kernel<DT>, grid_of(a.rows), dim3(1024), 0, s, a);
     }
-    if (a.dweight) hipLaunchKernelGGL(norm_dweight_sum_kernel, dim3((unsigned)ceil_div(a.cols, 32)), dim3(32 * kShares), 0, s, p);
+    if (a.dweight) hipLaunchKernelGGL(norm_dweight_sum_kernel, grid_of(ceil_div(a.cols, 32)), dim3(32 * kShares), 0, s, p);
     return launch_status();
 }
 

@@ -193,3 +193,53 @@ def test_sources_and_results_past_32_bits(hb):
     y = hb.gemm_mx4(a, b, dtype=BF16)
     want = hb.read_mx4(a)[rows - 50:].double() @ hb.read_mx4(b).double().t().contiguous()
     assert bool(((y[rows - 50:].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -15).all())       # (sums of 64 products: below 2^8, exact but for the rounding)
+
+
+def test_norms_of_more_rows_than_a_row_of_workgroups(hb):
+    """More than 2^21 workgroups: the rows behind them against the same ones alone."""
+    rows, cols = 4 * (1 << 21) + 9, 3
+    x = torch.randn((rows, cols), generator=torch.Generator(device="cuda").manual_seed(21), device="cuda").to(BF16)
+    for at in (0, rows - 40, 4 * (1 << 21) - 20):
+        part = x[at:at + 30].contiguous()
+        for norm in (hb.norm_i8, hb.norm_mx4):
+            (all_of, _, rstd, values), (some, _, some_rstd, some_values) = norm(x, None, values=True), norm(part, None, values=True)
+            assert torch.equal(rstd[at:at + 30], some_rstd) and torch.equal(values[at:at + 30], some_values)
+            if norm is hb.norm_mx4:
+                assert torch.equal(all_of.codes[:, at:at + 30], some.codes) and torch.equal(all_of.scales[:, at:at + len(part)], some.scales[:, :len(part)])
+            del all_of, rstd, values
+
+
+def test_conversions_of_more_rows_than_a_row_of_workgroups(hb):
+    rows, cols = 32 * (1 << 21) + 40, 2
+    x = torch.randn((rows, cols), generator=torch.Generator(device="cuda").manual_seed(22), device="cuda")
+    t = hb.quant_mx4(x)
+    values = hb.read_mx4(t)
+    for at in (0, 32 * (1 << 21) - 20, rows - 30):
+        some = hb.quant_mx4(x[at:at + 30].contiguous())
+        assert torch.equal(t.codes[:, at:at + 30], some.codes) and torch.equal(t.scales[:, at:at + 30], some.scales[:, :30])
+        assert torch.equal(values[at:at + 30], hb.read_mx4(some))
+
+
+def test_a_token_and_more_outputs_than_a_row_of_workgroups(hb):
+    n, k = 16 * (1 << 21) + 20, 40
+    w = torch.randn((n, k), generator=torch.Generator(device="cuda").manual_seed(23), device="cuda")
+    x = torch.randn((1, k), generator=torch.Generator(device="cuda").manual_seed(24), device="cuda")
+    y = hb.linear_mx4(x, hb.quant_mx4(w))
+    for at in (0, 16 * (1 << 21) - 20, n - 30):
+        assert torch.equal(y[:, at:at + 30], hb.linear_mx4(x, hb.quant_mx4(w[at:at + 30].contiguous())))
+
+
+def test_gradient_of_a_row_of_more_columns_than_a_row_of_workgroups(hb):
+    """One row: its dweight is one product of two roundings; its dx is rstd g, for the mean of g u is nothing here."""
+    cols = 32 * (1 << 21) + 40
+    s = torch.randn((1, cols // 2), generator=torch.Generator(device="cuda").manual_seed(25), device="cuda")
+    s, g = torch.cat((s, s), 1), torch.ones((1, cols), device="cuda")
+    g[:, cols // 2:] = -1.0
+    r = torch.full((1,), 0.5, device="cuda")
+    dx, dw = hb.norm_grad(g, s, r, None)
+    assert torch.equal(dw, (g * (s * 0.5))[0])
+    # a sum of `cols` terms of magnitude |u|, at most cols additions deep in 1024 shares and 1023 more: off by (cols / 1024 + 1024 + 8) 2^-24 of the
+    # sum of |u| at most, and the mean by as much of the mean of |u| (1 % for terms of second order); two roundings of values near 1 in dx
+    u = (0.5 * s).abs()
+    mean = 1.01 * (cols / 1024 + 1032) * 2.0 ** -24 * u.double().mean().item()
+    assert bool(((dx - 0.5 * g).abs() <= 0.5 * mean * u + 2.0 ** -23).all())

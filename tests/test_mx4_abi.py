@@ -85,6 +85,27 @@ def test_product_refusals():
     assert linear(y=None) == hbfp.ERR_ARG and linear(y=P + 2 * FAR) == hbfp.ERR_ARG and linear(size=need - 1) == hbfp.ERR_WORKSPACE
 
 
+def test_more_tiles_than_a_launch_holds_are_refused_before_anything_is_queued():
+    most, far = (1 << 31) - 1, 1 << 42
+
+    def op(rows, kdim, at):
+        d = hbfp.mx4_plan(rows, kdim)
+        d.codes, d.scales = at, at + d.code_bytes + (-d.code_bytes) % 256
+        return d
+
+    n = ctypes.c_size_t(0)
+    a, b = op(most, 64, far), op(17, 64, P)
+    assert L.hbfp_gemm_mx4_workspace(most, 17, 64, ref(n)) == hbfp.OK and n.value == 0
+    assert L.hbfp_gemm_mx4(ref(a), ref(b), None, 2 * far, 1, 17, None, 0, None) == hbfp.ERR_ARG
+    assert L.hbfp_gemm_mx4(ref(b), ref(a), None, 2 * far, 1, most, None, 0, None) == hbfp.ERR_ARG
+    assert L.hbfp_linear_mx4_workspace(most, 17, 64, ref(n)) == hbfp.OK
+    assert L.hbfp_linear_mx4(2 * far, 1, most, 64, ref(b), None, 3 * far, 17, far, n.value, None) == hbfp.ERR_ARG
+    rows = 0x7fffff00
+    along, down = op(rows, 200, 2 * far), op(200, rows, far)
+    assert L.hbfp_quant_mx4(3 * far, 1, rows, 200, 200, 0, 0, None, ref(down), None) == hbfp.ERR_ARG
+    assert L.hbfp_quant_mx4(3 * far, 1, rows, 200, 200, 0, 0, ref(along), ref(down), None) == hbfp.ERR_ARG
+
+
 def test_linear_refuses_to_write_the_tokens_it_still_reads():
     w = _op(256, 256, P + 2 * FAR)
     lin = lambda x, y, m, ldx, ldy: L.hbfp_linear_mx4(x, 1, m, ldx, ref(w), None, y, ldy, None, 0, None)
