@@ -335,7 +335,7 @@ __global__ __launch_bounds__(64 * W) void gemm_mx4_few_kernel(const Mx4FewParams
                 const int64_t left = K - k;
                 load8<DT>(p.x, m * p.ldx + k, left < 8 ? (int)(left < 0 ? 0 : left) : 8, x);
                 const uint32_t byte = mx4_byte<HBFP_RNE>(largest_of_quad(mx4_largest8(x)));
-                *reinterpret_cast<uint32_t *>(own + m * row_bytes + k / 2) = mx4_codes8(x, byte);
+                *reinterpret_cast<uint32_t *>(own + m * row_bytes + k / 2) = mx4_codes<8>(x, byte);
                 if (t % 4 == 0) own_scales[(m * row_bytes + k / 2) / 16] = (uint8_t)byte;
             }
         }

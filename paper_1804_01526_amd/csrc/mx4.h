@@ -72,15 +72,18 @@ __device__ __forceinline__ uint32_t mx4_byte(uint32_t amax) {
     return e < 2u ? 0u : e - 2u;
 }
 
-// eight values -> a word of codes, to nearest.  The instruction divides by a power of two of which it reads the exponent field alone
+// eight values -> a word of codes, four or two -> a half or a quarter of one, to nearest.  The instruction divides by a power of two of which it reads the exponent field alone
 // (0: 2^-127), rounds to nearest even and cuts at 6; the builtin writes one byte of the word.
-__device__ __forceinline__ uint32_t mx4_codes8(const float *x, uint32_t byte) {
+template <int C>
+__device__ __forceinline__ uint32_t mx4_codes(const float *x, uint32_t byte) {
     const float unit = __uint_as_float(byte << 23);
     uint32_t w = 0;
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], unit, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], unit, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], unit, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], unit, 3);
+    if constexpr (C >= 4) w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], unit, 1);
+    if constexpr (C == 8) {
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], unit, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], unit, 3);
+    }
     return byte == 255u ? 0u : w;
 }
 

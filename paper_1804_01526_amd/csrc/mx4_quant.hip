@@ -17,26 +17,27 @@ struct QuantMx4Params {
     int32_t eights;              // rows of a multiple of eight values
 };
 
-// the random words of eight neighbours from position `at` on.  Where rows are multiples of eight, so is `at`, and the hash's first steps, which are
+// the random words of C neighbours from position `at` on.  Where rows are multiples of eight, `at` is one of C, and the hash's first steps, which are
 // linear over bits, are taken once for all of them (4096 x 4096 bf16 along 21.8 -> 19.8 us, both 33.8 -> 31.7)
-__device__ __forceinline__ void random_words8(uint64_t at, const QuantMx4Params &p, uint32_t *h) {
+template <int C>
+__device__ __forceinline__ void random_words(uint64_t at, const QuantMx4Params &p, uint32_t *h) {
     if (p.eights) {
         const uint32_t first = sr_triple((uint32_t)at ^ p.s0), high = (uint32_t)(at >> 32) ^ p.s1;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = sr_hash_tail(first ^ sr_triple(i), high);
+        for (int i = 0; i < C; ++i) h[i] = sr_hash_tail(first ^ sr_triple(i), high);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = sr_hash((uint32_t)(at + i), (uint32_t)((at + i) >> 32), p.s0, p.s1);
+        for (int i = 0; i < C; ++i) h[i] = sr_hash((uint32_t)(at + i), (uint32_t)((at + i) >> 32), p.s0, p.s1);
     }
 }
 
 template <int ROUND>
 __device__ __forceinline__ uint32_t codes8(const float *x, uint32_t byte, int64_t idx, const QuantMx4Params &p) {
     if constexpr (ROUND == HBFP_RNE) {
-        return mx4_codes8(x, byte);
+        return mx4_codes<8>(x, byte);
     } else {
         uint32_t w = 0, h[8];
-        random_words8((uint64_t)idx, p, h);
+        random_words<8>((uint64_t)idx, p, h);
 #pragma unroll
         for (int i = 0; i < 8; ++i) w |= mx4_code_sr(x[i], byte, h[i]) << (4 * i);
         return byte == 255u ? 0u : w;
@@ -68,10 +69,10 @@ __global__ __launch_bounds__(256) void quant_mx4_along_kernel(const QuantMx4Para
     }
 }
 
-// ---- down the columns, or both.  A workgroup has a tile of 128 x 128, a thread 8 x 8 of it: four neighbouring lanes share the blocks along
-// its rows, and the four lanes 16 apart of a wave those down its columns, so that both maxima are found between lanes and a random word serves both
-// codes of its value (with values that meet in LDS and are rounded by each side for itself, stochastic 4096 x 4096 took 44 us, 1001 x 777 31 instead of 13).
-// The words of the columns meet in LDS, from where four threads store 64 bytes of a column's codes.
+// ---- down the columns, or both.  A workgroup has a tile of 128 rows and 16 C columns, a thread 8 rows and C columns of it: 32 / C neighbouring lanes
+// share the blocks along its rows, and the four lanes 16 apart of a wave those down its columns, so that both maxima are found between lanes and a random
+// word serves both codes of its value (with values that meet in LDS and are rounded by each side for itself, stochastic 4096 x 4096 took 44 us, 1001 x 777
+// 31 instead of 13).  The words of the columns meet in LDS, from where four threads store 64 bytes of a column's codes.
 
 // largest of the lanes l, l ^ 16, l ^ 32, l ^ 48: two exchanges of rows of lanes on the vector unit
 __device__ __forceinline__ uint32_t largest_of_column(uint32_t x) {
@@ -80,33 +81,76 @@ __device__ __forceinline__ uint32_t largest_of_column(uint32_t x) {
     const v2u b = __builtin_bit_cast(v2u, __builtin_amdgcn_permlane16_swap(x, x, false, false));
     return b[0] > b[1] ? b[0] : b[1];
 }
+// ... of the 32 / C neighbouring lanes of a block
+template <int C>
+__device__ __forceinline__ uint32_t largest_of_block(uint32_t x) {
+    x = largest_of_quad(x);
+    if constexpr (C <= 4) {
+        const uint32_t y = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xF, 0xF, true);      // lanes 7, 6, ... 0
+        x = y > x ? y : x;
+    }
+    if constexpr (C == 2) {
+        const uint32_t y = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x140, 0xF, 0xF, true);      // lanes 15, 14, ... 0
+        x = y > x ? y : x;
+    }
+    return x;
+}
 
-template <int DT, int ROUND, bool ALONG>
-__global__ __launch_bounds__(256, ALONG && ROUND == HBFP_STOCHASTIC ? 3 : 4) void quant_mx4_down_kernel(const QuantMx4Params p) {
-    __shared__ __attribute__((aligned(16))) uint32_t words[128][20];     // 16 of column 8 a + b in row 16 b + a: a wave's writes cover all banks
+// C neighbours from element i on, of which n (may be <= 0) exist
+template <int DT, int C>
+__device__ __forceinline__ void load_some(const void *p, int64_t i, int64_t n, float *x) {
+    if constexpr (C == 8) {
+        load8<DT>(p, i, n < 0 ? 0 : n < 8 ? (int)n : 8, x);
+    } else if (n < C) {
+#pragma unroll
+        for (int j = 0; j < C; ++j) x[j] = j < n ? load_as_float<DT>(p, i + j) : 0.0f;
+    } else if constexpr (DT == HBFP_F32) {
+        typedef float floats_at __attribute__((ext_vector_type(C), aligned(4)));
+        const floats_at a = *reinterpret_cast<const floats_at *>(reinterpret_cast<const float *>(p) + i);
+#pragma unroll
+        for (int j = 0; j < C; ++j) x[j] = a[j];
+    } else {
+        typedef uint16_t halves_at __attribute__((ext_vector_type(C), aligned(2)));
+        const halves_at a = *reinterpret_cast<const halves_at *>(reinterpret_cast<const uint16_t *>(p) + i);
+#pragma unroll
+        for (int j = 0; j < C; ++j) x[j] = DT == HBFP_BF16 ? __uint_as_float((uint32_t)a[j] << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)a[j]);
+    }
+}
+template <int C>
+__device__ __forceinline__ uint32_t largest_of(const float *x) {
+    uint32_t amax = 0;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const uint32_t a = __float_as_uint(x[i]) & 0x7fffffffu;
+        amax = a > amax ? a : amax;
+    }
+    return amax;
+}
+
+template <int DT, int ROUND, bool ALONG, int C>
+__global__ __launch_bounds__(256, ALONG && ROUND == HBFP_STOCHASTIC && C == 8 ? 3 : 4) void quant_mx4_down_kernel(const QuantMx4Params p) {
+    constexpr int kWide = 16 * C;
+    __shared__ __attribute__((aligned(16))) uint32_t words[kWide][20];   // 16 of column C a + b in row 16 b + a: a wave's writes cover all banks
     const int t = threadIdx.x, lane = t & 63, tr = t / 16;
     // workgroups are dealt to the 8 XCDs in turn: each gets a run of tiles, two rows of them side by side, so that the halves of a line of codes
     // of either operand meet in one L2 (16384 x 16384 bf16, both: 219 us by rows of tiles over all XCDs, 190 so; 4096 x 4096 13.4 and 13.7)
     const uint32_t tile = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
     if (tile >= p.tiles) return;
     const uint32_t band = tile / (2 * p.tiles_c), in_band = tile - band * 2 * p.tiles_c;
-    const int64_t c0 = (int64_t)(in_band >> 1) * 128, r0 = ((int64_t)band * 2 + (in_band & 1)) * 128;
-    const int64_t c = c0 + 8 * (t % 16), r = r0 + 8 * tr, left = p.cols - c;
-    float x[8][8];
+    const int64_t c0 = (int64_t)(in_band >> 1) * kWide, r0 = ((int64_t)band * 2 + (in_band & 1)) * 128;
+    const int64_t c = c0 + C * (t % 16), r = r0 + 8 * tr, left = p.cols - c;
+    float x[8][C];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) load8<DT>(p.src, (r + i) * p.ld + c, r + i >= p.rows || left <= 0 ? 0 : left < 8 ? (int)left : 8, x[i]);
-    uint32_t down[8];                                       // bytes of the columns' blocks
+    for (int i = 0; i < 8; ++i) load_some<DT, C>(p.src, (r + i) * p.ld + c, r + i >= p.rows ? 0 : left, x[i]);
+    uint32_t down[C];                                       // bytes of the columns' blocks
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        uint32_t amax = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t a = __float_as_uint(x[i][j]) & 0x7fffffffu;
-            amax = a > amax ? a : amax;
-        }
-        down[j] = mx4_byte<ROUND>(largest_of_column(amax));
+    for (int j = 0; j < C; ++j) {
+        const float y[8] = {x[0][j], x[1][j], x[2][j], x[3][j], x[4][j], x[5][j], x[6][j], x[7][j]};
+        down[j] = mx4_byte<ROUND>(largest_of_column(mx4_largest8(y)));
     }
-    uint32_t column[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    uint32_t column[C];
+#pragma unroll
+    for (int j = 0; j < C; ++j) column[j] = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         // one row after the other: side by side they would take 256 registers
@@ -114,38 +158,41 @@ __global__ __launch_bounds__(256, ALONG && ROUND == HBFP_STOCHASTIC ? 3 : 4) voi
         uint64_t at = (uint64_t)(r + i) * (uint64_t)p.cols + (uint64_t)c;
         asm volatile("" : "+v"(at));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(x[i][j]));
+        for (int j = 0; j < C; ++j) asm volatile("" : "+v"(x[i][j]));
         uint32_t byte = 0, w = 0;
-        if constexpr (ALONG) byte = mx4_byte<ROUND>(largest_of_quad(mx4_largest8(x[i])));
+        if constexpr (ALONG) byte = mx4_byte<ROUND>(largest_of_block<C>(largest_of<C>(x[i])));
         if constexpr (ROUND == HBFP_RNE) {
-            if constexpr (ALONG) w = mx4_codes8(x[i], byte);
+            if constexpr (ALONG) w = mx4_codes<C>(x[i], byte);
         } else {
-            uint32_t h[8];
-            random_words8(at, p, h);
+            uint32_t h[C];
+            random_words<C>(at, p, h);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < C; ++j) {
                 if constexpr (ALONG) w |= mx4_code_sr(x[i][j], byte, h[j]) << (4 * j);
                 column[j] |= mx4_code_sr(x[i][j], down[j], h[j]) << (4 * i);
             }
             if (byte == 255u) w = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(column[j]));
+            for (int j = 0; j < C; ++j) asm volatile("" : "+v"(column[j]));
             asm volatile("" : "+v"(w));
         }
         if constexpr (ALONG) {
             if (r + i < p.rows) {
-                const int64_t line = (c0 >> 8) * p.rows + r + i;
-                reinterpret_cast<uint32_t *>(p.along.codes + line * 128 + ((c0 & 255) >> 1))[t % 16] = w;
-                if (t % 4 == 0) p.along.scales[((c0 >> 8) * p.along.scale_rows + r + i) * 8 + ((c0 & 255) >> 5) + (t % 16) / 4] = (uint8_t)byte;
+                uint8_t *const line = p.along.codes + ((c0 >> 8) * p.rows + r + i) * 128 + ((c0 & 255) >> 1);
+                if constexpr (C == 8) reinterpret_cast<uint32_t *>(line)[t % 16] = w;
+                else if constexpr (C == 4) reinterpret_cast<uint16_t *>(line)[t % 16] = (uint16_t)w;
+                else line[t % 16] = (uint8_t)w;
+                if (t % (32 / C) == 0)
+                    p.along.scales[((c0 >> 8) * p.along.scale_rows + r + i) * 8 + ((c0 & 255) >> 5) + (t % 16) / (32 / C)] = (uint8_t)byte;
             }
         }
     }
     const int64_t group = r0 >> 8;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < C; ++j) {
         if constexpr (ROUND == HBFP_RNE) {
             const float y[8] = {x[0][j], x[1][j], x[2][j], x[3][j], x[4][j], x[5][j], x[6][j], x[7][j]};
-            column[j] = mx4_codes8(y, down[j]);
+            column[j] = mx4_codes<8>(y, down[j]);
         } else {
             if (down[j] == 255u) column[j] = 0;
         }
@@ -154,14 +201,33 @@ __global__ __launch_bounds__(256, ALONG && ROUND == HBFP_STOCHASTIC ? 3 : 4) voi
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int col = 8 * (lane / 4) + t / 64 + 4 * i;     // (columns 8 apart: neighbouring rows of words, every bank once)
-        if (c0 + col < p.cols)
+    for (int i = 0; i < (C + 2) / 4; ++i) {
+        const int col = C * (lane / 4) + t / 64 + 4 * i;     // (columns C apart: neighbouring rows of words, every bank once)
+        if ((C > 2 || t < 128) && c0 + col < p.cols)
             *reinterpret_cast<v4u *>(p.down.codes + (group * p.cols + c0 + col) * 128 + ((r0 & 255) >> 1) + 16 * (t % 4)) =
-                *reinterpret_cast<const v4u *>(&words[16 * (col % 8) + col / 8][4 * (t % 4)]);
+                *reinterpret_cast<const v4u *>(&words[16 * (col % C) + col / C][4 * (t % 4)]);
     }
 }
 
+template <int DT, int ROUND, int C>
+int launch_down(QuantMx4Params p, bool along, hipStream_t s) {
+    // whole groups of whichever operands are wanted: what is past the source is stored as zeros
+    const int64_t tiles_c = along ? 16 / C * p.along.groups : ceil_div(p.cols, 16 * C), wgs = tiles_c * 2 * p.down.groups;
+    if (!one_row(round_up(wgs, 8), 256)) return HBFP_ERR_ARG;
+    p.tiles_c = (uint32_t)tiles_c;
+    p.tiles = (uint32_t)wgs;
+    void (*const kernel)(QuantMx4Params) = along ? &quant_mx4_down_kernel<DT, ROUND, true, C> : &quant_mx4_down_kernel<DT, ROUND, false, C>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)round_up(wgs, 8)), dim3(256), 0, s, p);
+    return launch_status();
+}
+
+// Columns of a thread: fewer where the matrix has too few tiles to keep the chip's vector units busy.  us with 8, 4 and 2 of both operands, stochastic (bf16):
+// 501 x 730 13.8, 9.1, 6.9; 1024 x 1024 (64 tiles) 11.0, 7.8, 6.7; 1024 x 2048 11.2, 8.1, 8.1; 2048 x 2048 12.0, 11.1, 11.7; 2048 x 4096 17.3, 17.1;
+// 4096 x 4096 30.4, 30.9; to nearest 6.1, 5.3, 5.1 of 1024 x 1024, 8.1, 8.1 of 2048 x 4096, 13.1, 14.0 of 4096 x 4096
+int down_columns(const QuantMx4Params &p, bool along) {
+    const int64_t tiles = (along ? 2 * p.along.groups : ceil_div(p.cols, 128)) * 2 * p.down.groups;
+    return tiles <= 64 ? 2 : tiles <= 512 ? 4 : 8;
+}
 template <int DT, int ROUND>
 int launch_quant(QuantMx4Params p, bool along, bool down, hipStream_t s) {
     if (!down) {
@@ -171,15 +237,8 @@ int launch_quant(QuantMx4Params p, bool along, bool down, hipStream_t s) {
         hipLaunchKernelGGL((quant_mx4_along_kernel<DT, ROUND>), grid_of(wgs), dim3(256), 0, s, p);
         return launch_status();
     }
-    // whole groups of whichever operands are wanted: what is past the source is stored as zeros
-    const int64_t tiles_c = along ? 2 * p.along.groups : ceil_div(p.cols, 128), tiles_r = 2 * p.down.groups;
-    const int64_t wgs = tiles_c * tiles_r;
-    if (!one_row(round_up(wgs, 8), 256)) return HBFP_ERR_ARG;
-    p.tiles_c = (uint32_t)tiles_c;
-    p.tiles = (uint32_t)wgs;
-    void (*const kernel)(QuantMx4Params) = along ? &quant_mx4_down_kernel<DT, ROUND, true> : &quant_mx4_down_kernel<DT, ROUND, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)round_up(wgs, 8)), dim3(256), 0, s, p);
-    return launch_status();
+    const int wide = down_columns(p, along);
+    return wide == 2 ? launch_down<DT, ROUND, 2>(p, along, s) : wide == 4 ? launch_down<DT, ROUND, 4>(p, along, s) : launch_down<DT, ROUND, 8>(p, along, s);
 }
 
 // ---- back.  A workgroup has 32 rows of one group; a thread a word of eight codes in four of them, all loads first.  8192 x 4096 as bf16: 13 to 15 us,

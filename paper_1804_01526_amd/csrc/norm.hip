@@ -96,7 +96,7 @@ __device__ __forceinline__ void put_i8(const NormArgs &a, int64_t row, int64_t c
 template <int DT>
 __device__ __forceinline__ void put_mx4(const NormArgs &a, int64_t row, int64_t c, int left, const float *n, int lane) {
     const uint32_t byte = mx4_byte<HBFP_RNE>(largest_of_quad(mx4_largest8(n)));
-    const uint32_t w = mx4_codes8(n, byte);
+    const uint32_t w = mx4_codes<8>(n, byte);
     const int64_t group = c >> 8;
     if (group >= a.mx4.groups) return;
     *reinterpret_cast<uint32_t *>(a.mx4.codes + (group * a.mx4.rows + row) * 128 + ((c & 255) >> 1)) = w;

@@ -10,6 +10,7 @@ import pytest
 import torch
 
 from tests import mx4_ref
+from tests.util import launched_kernels
 
 pytestmark = pytest.mark.gpu
 
@@ -78,6 +79,37 @@ def test_quant_holds_the_definition_s_codes(hb, rows, cols, ld, dtype, rounding)
         want = mx4_ref.held(n, None if h is None else h if t is along else h.T)
         for out_type in (F32, BF16):
             np.testing.assert_array_equal(_np(hb.read_mx4(t, out_type)), want)
+
+
+@pytest.mark.parametrize("rows,cols,ld,wide", [(501, 731, 733, 2), (512, 1000, 1000, 2), (1001, 2304, 2304, 4), (2003, 2307, 2311, 4), (3001, 5003, 5003, 8),
+                                               (4096, 4104, 4104, 8)])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rounding", [0, 1])
+def test_kernels_of_the_conversion(hb, rows, cols, ld, wide, dtype, rounding):
+    """Threads of two, four and eight columns: the codes of whole matrices against the conversion along the rows, some of them against the definition."""
+    print(f"[conversion] {rows}x{cols} ld {ld} {dtype} rounding {rounding}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.full((rows, ld), float("nan"), dtype=dtype, device="cuda")[:, :cols]
+    x.copy_(torch.randn((rows, cols), generator=gen, device="cuda"))
+    x[rows // 2, cols // 2], x[rows - 2, 3], x[5, cols - 1] = float("inf"), float("nan"), float("-inf")
+    seed, d = 0xFEDCBA9876543210, {F32: 0, BF16: 1, F16: 2}[dtype]
+    held = {}
+    assert launched_kernels(lambda: held.update(both=hb.quant_mx4_both(x, rounding, seed))) == [f"quant_mx4_down_kernel<{d}, {rounding}, true, {wide}>"]
+    assert launched_kernels(lambda: held.update(down=hb.quant_mx4(x, 0, rounding, seed))) == [f"quant_mx4_down_kernel<{d}, {rounding}, false, {wide}>"]
+    (along, down), alone, across = held["both"], held["down"], hb.quant_mx4(x, 1, rounding, seed)
+    same = lambda t, u: torch.equal(t.codes, u.codes) and torch.equal(t.scales[:, :t.desc.rows], u.scales[:, :u.desc.rows])
+    assert same(along, across) and same(down, alone)
+    if not rounding:
+        assert same(down, hb.quant_mx4(x.t().contiguous()))
+    for t, n, m, source in ((along, rows, cols, x), (down, cols, rows, x.t())):
+        picked = np.unique(np.r_[0:9, n // 2 - 20:n // 2 + 20, n - 20:n])
+        here = torch.from_numpy(picked).cuda()
+        at = picked[:, None].astype(np.uint64) * np.uint64(m) + np.arange(m, dtype=np.uint64) if t is along else \
+            np.arange(m, dtype=np.uint64) * np.uint64(n) + picked[:, None].astype(np.uint64)
+        codes, scales = mx4_ref.quant(_np(source[here]), mx4_ref.words_at(at, seed) if rounding else None)
+        got_codes, got_scales = (v[picked] for v in _stored(t))
+        np.testing.assert_array_equal(got_scales, scales)
+        _same_codes(got_codes, codes)
 
 
 def test_quant_at_the_ends(hb):
