@@ -1,8 +1,8 @@
 // Conversion of a matrix into microscaled 4-bit operands, along its rows, down its columns or both from one read, and back.
-// Bound by memory: a value costs its bytes once and 17/32 byte for each operand.  4096 x 4096 along the rows: bf16 8.3 us (5.1 TB/s), FP32 13.3
-// (5.7); down the columns 10.1 and 14.3; both 13.7 and 17.1 (3.8 and 5.0), where the two calls would take 18.4 and 27.6.  Stochastic rounding is bound
-// by the vector unit, some 37 instructions a value for the first operand and 18 for the second, two of them 32-bit multiplications at a quarter
-// of the rate: bf16 along 19.8 us, both 31.7.
+// Bound by memory: a value costs its bytes once and 17/32 byte for each operand.  4096 x 4096 along the rows: bf16 8.9 us (4.8 TB/s), FP32 12.9
+// (5.9); down the columns 10.1 and 14.3; both 13.7 and 17.1 (3.8 and 5.0), where the two calls would take 19.0 and 27.2.  Stochastic rounding is bound
+// by the vector unit, 54 instructions a value for both operands, two of them 32-bit multiplications at a quarter of the rate: bf16 along
+// 18.7 us, both 31.
 #include "mx4.h"
 
 namespace hbfp {
@@ -18,7 +18,7 @@ struct QuantMx4Params {
 };
 
 // the random words of C neighbours from position `at` on.  Where rows are multiples of eight, `at` is one of C, and the hash's first steps, which are
-// linear over bits, are taken once for all of them (4096 x 4096 bf16 along 21.8 -> 19.8 us, both 33.8 -> 31.7)
+// linear over bits, are taken once for all of them (4096 x 4096 bf16 along 21.8 -> 19.8 us, both 33.8 -> 31.7, with four rows a thread)
 template <int C>
 __device__ __forceinline__ void random_words(uint64_t at, const QuantMx4Params &p, uint32_t *h) {
     if (p.eights) {
@@ -44,22 +44,22 @@ __device__ __forceinline__ uint32_t codes8(const float *x, uint32_t byte, int64_
     }
 }
 
-// ---- along the rows alone.  A workgroup has 32 rows of one group of 256: a thread converts 8 neighbours of 4 rows, all loads first;
+// ---- along the rows alone.  A workgroup has 8 N rows of one group of 256: a thread converts 8 neighbours of N rows, all loads first;
 // four lanes are a block, 32 lanes a line of codes.
-template <int DT, int ROUND>
+template <int DT, int ROUND, int N>
 __global__ __launch_bounds__(256) void quant_mx4_along_kernel(const QuantMx4Params p) {
     const int t = threadIdx.x;
-    const int64_t group = workgroup() % p.tiles_c, r0 = (int64_t)(workgroup() / p.tiles_c) * 32 + t / 32;
+    const int64_t group = workgroup() % p.tiles_c, r0 = (int64_t)(workgroup() / p.tiles_c) * (8 * N) + t / 32;
     const int64_t c = group * 256 + 8 * (t % 32);
     const int64_t left = p.cols - c;
-    float x[4][8];
+    float x[N][8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N; ++i) {
         const int64_t r = r0 + 8 * i;
         load8<DT>(p.src, r * p.ld + c, r >= p.rows || left <= 0 ? 0 : left < 8 ? (int)left : 8, x[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N; ++i) {
         const int64_t r = r0 + 8 * i;
         const uint32_t byte = mx4_byte<ROUND>(largest_of_quad(mx4_largest8(x[i])));
         const uint32_t w = codes8<ROUND>(x[i], byte, r * p.cols + c, p);
@@ -221,6 +221,21 @@ int launch_down(QuantMx4Params p, bool along, hipStream_t s) {
     return launch_status();
 }
 
+// Rows of a thread, of the kernels that go along the rows: one where they are few, else two.  us with 1, 2 and 4, conversion to nearest and stochastically and
+// reading back, of bf16: 64 x 4096 3.1, 3.3, 3.6; 3.4, 3.9, 5.2; 2.9, 3.0, 3.2; 1024 x 1024 (512 workgroups of one row a thread) 3.0, 3.2, 3.7; 4.0, 4.1, 5.3; 3.1,
+// 3.2, 3.5; 512 x 8192 3.9, 3.9, 4.1; 7.9, 6.6, 7.1; 4.3, 4.4, 4.5; 4096 x 4096 9.5, 8.9, 8.2; 23.3, 18.7, 19.5; 8.5, 8.5, 8.4; 8192 x 8192 -, 26.2, 32.0;
+// -, 59.0, 62.2; 26.5, 26.5, 29.0; 16384 x 16384 -, 112, 115; -, 225, 223; 168, 129, 135
+bool few_lines(const Mx4View &t) { return t.groups * ceil_div(t.rows, 8) <= 512; }
+
+template <int DT, int ROUND, int N>
+int launch_along(QuantMx4Params p, hipStream_t s) {
+    p.tiles_c = (uint32_t)p.along.groups;
+    const int64_t wgs = p.along.groups * ceil_div(p.rows, 8 * N);
+    if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
+    hipLaunchKernelGGL((quant_mx4_along_kernel<DT, ROUND, N>), grid_of(wgs), dim3(256), 0, s, p);
+    return launch_status();
+}
+
 // Columns of a thread: fewer where the matrix has too few tiles to keep the chip's vector units busy.  us with 8, 4 and 2 of both operands, stochastic (bf16):
 // 501 x 730 13.8, 9.1, 6.9; 1024 x 1024 (64 tiles) 11.0, 7.8, 6.7; 1024 x 2048 11.2, 8.1, 8.1; 2048 x 2048 12.0, 11.1, 11.7; 2048 x 4096 17.3, 17.1;
 // 4096 x 4096 30.4, 30.9; to nearest 6.1, 5.3, 5.1 of 1024 x 1024, 8.1, 8.1 of 2048 x 4096, 13.1, 14.0 of 4096 x 4096
@@ -231,33 +246,28 @@ int down_columns(const QuantMx4Params &p, bool along) {
 template <int DT, int ROUND>
 int launch_quant(QuantMx4Params p, bool along, bool down, hipStream_t s) {
     if (!down) {
-        p.tiles_c = (uint32_t)p.along.groups;
-        const int64_t wgs = p.along.groups * ceil_div(p.rows, 32);
-        if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
-        hipLaunchKernelGGL((quant_mx4_along_kernel<DT, ROUND>), grid_of(wgs), dim3(256), 0, s, p);
-        return launch_status();
+        return few_lines(p.along) ? launch_along<DT, ROUND, 1>(p, s) : launch_along<DT, ROUND, 2>(p, s);
     }
     const int wide = down_columns(p, along);
     return wide == 2 ? launch_down<DT, ROUND, 2>(p, along, s) : wide == 4 ? launch_down<DT, ROUND, 4>(p, along, s) : launch_down<DT, ROUND, 8>(p, along, s);
 }
 
-// ---- back.  A workgroup has 32 rows of one group; a thread a word of eight codes in four of them, all loads first.  8192 x 4096 as bf16: 13 to 15 us,
-// 5.6 to 6.4 TB/s.
-template <int DT>
+// ---- back.  A workgroup has 8 N rows of one group; a thread a word of eight codes in N of them, all loads first.  8192 x 4096 as bf16: 14.5 us, 5.9 TB/s.
+template <int DT, int N>
 __global__ __launch_bounds__(256) void read_mx4_kernel(const Mx4View t, void *dst, int64_t ld) {
-    const int64_t group = workgroup() % (uint32_t)t.groups, r0 = (int64_t)(workgroup() / (uint32_t)t.groups) * 32 + threadIdx.x / 32;
+    const int64_t group = workgroup() % (uint32_t)t.groups, r0 = (int64_t)(workgroup() / (uint32_t)t.groups) * (8 * N) + threadIdx.x / 32;
     const int at = threadIdx.x % 32;
     const int64_t k = group * 256 + 8 * at, left = t.kdim - k;
     if (left <= 0) return;
-    uint32_t w[4], byte[4];
+    uint32_t w[N], byte[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N; ++i) {
         const int64_t r = r0 + 8 * i < t.rows ? r0 + 8 * i : t.rows - 1;
         w[i] = reinterpret_cast<const uint32_t *>(t.codes + (group * t.rows + r) * 128)[at];
         byte[i] = t.scales[(group * t.scale_rows + r) * 8 + at / 4];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N; ++i) {
         const int64_t r = r0 + 8 * i;
         if (r >= t.rows) return;
         if (DT == HBFP_BF16 && left >= 8) {
@@ -269,6 +279,18 @@ __global__ __launch_bounds__(256) void read_mx4_kernel(const Mx4View t, void *ds
         store4<DT>(dst, r * ld + k, left < 4 ? (int)left : 4, x);
         store4<DT>(dst, r * ld + k + 4, left < 8 ? (int)left - 4 : 4, x + 4);
     }
+}
+
+template <int DT, int N>
+int launch_read(const Mx4View &t, void *dst, int64_t ld, hipStream_t s) {
+    const int64_t wgs = t.groups * ceil_div(t.rows, 8 * N);
+    if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
+    hipLaunchKernelGGL((read_mx4_kernel<DT, N>), grid_of(wgs), dim3(256), 0, s, t, dst, ld);
+    return launch_status();
+}
+template <int DT>
+int launch_read_of(const Mx4View &t, void *dst, int64_t ld, hipStream_t s) {
+    return few_lines(t) ? launch_read<DT, 1>(t, dst, ld, s) : launch_read<DT, 2>(t, dst, ld, s);
 }
 
 template <int DT>
@@ -289,11 +311,7 @@ int launch_quant_mx4(const void *src, int dtype, int64_t rows, int64_t cols, int
 }
 
 int launch_read_mx4(const Mx4View &t, int dtype, void *dst, int64_t ld, hipStream_t s) {
-    const int64_t wgs = t.groups * ceil_div(t.rows, 32);
-    if (wgs > 0x7fffffff) return HBFP_ERR_ARG;
-    if (dtype == HBFP_F32) hipLaunchKernelGGL(read_mx4_kernel<HBFP_F32>, grid_of(wgs), dim3(256), 0, s, t, dst, ld);
-    else hipLaunchKernelGGL(read_mx4_kernel<HBFP_BF16>, grid_of(wgs), dim3(256), 0, s, t, dst, ld);
-    return launch_status();
+    return dtype == HBFP_F32 ? launch_read_of<HBFP_F32>(t, dst, ld, s) : launch_read_of<HBFP_BF16>(t, dst, ld, s);
 }
 
 }  // namespace hbfp

@@ -86,7 +86,7 @@ def test_quant_holds_the_definition_s_codes(hb, rows, cols, ld, dtype, rounding)
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("rounding", [0, 1])
 def test_kernels_of_the_conversion(hb, rows, cols, ld, wide, dtype, rounding):
-    """Threads of two, four and eight columns: the codes of whole matrices against the conversion along the rows, some of them against the definition."""
+    """Threads of two, four and eight columns, of one and two rows: the codes of whole matrices against the conversion along the rows, some of them against the definition."""
     print(f"[conversion] {rows}x{cols} ld {ld} {dtype} rounding {rounding}", flush=True)
     gen = torch.Generator(device="cuda").manual_seed(rows)
     x = torch.full((rows, ld), float("nan"), dtype=dtype, device="cuda")[:, :cols]
@@ -96,11 +96,18 @@ def test_kernels_of_the_conversion(hb, rows, cols, ld, wide, dtype, rounding):
     held = {}
     assert launched_kernels(lambda: held.update(both=hb.quant_mx4_both(x, rounding, seed))) == [f"quant_mx4_down_kernel<{d}, {rounding}, true, {wide}>"]
     assert launched_kernels(lambda: held.update(down=hb.quant_mx4(x, 0, rounding, seed))) == [f"quant_mx4_down_kernel<{d}, {rounding}, false, {wide}>"]
-    (along, down), alone, across = held["both"], held["down"], hb.quant_mx4(x, 1, rounding, seed)
+    rows_a_thread = 1 if rows * cols < 512 * 8 * 256 else 2
+    assert launched_kernels(lambda: held.update(across=hb.quant_mx4(x, 1, rounding, seed))) == [f"quant_mx4_along_kernel<{d}, {rounding}, {rows_a_thread}>"]
+    (along, down), alone, across = held["both"], held["down"], held["across"]
     same = lambda t, u: torch.equal(t.codes, u.codes) and torch.equal(t.scales[:, :t.desc.rows], u.scales[:, :u.desc.rows])
     assert same(along, across) and same(down, alone)
     if not rounding:
         assert same(down, hb.quant_mx4(x.t().contiguous()))
+    for out_type in (F32, BF16):
+        assert launched_kernels(lambda: held.update(values=hb.read_mx4(along, out_type))) == [f"read_mx4_kernel<{int(out_type == BF16)}, {rows_a_thread}>"]
+        picked = np.unique(np.r_[0:9, rows // 2 - 20:rows // 2 + 20, rows - 20:rows])
+        codes, scales = (v[picked] for v in _stored(along))
+        np.testing.assert_array_equal(_np(held["values"])[picked], mx4_ref.values(codes, scales))
     for t, n, m, source in ((along, rows, cols, x), (down, cols, rows, x.t())):
         picked = np.unique(np.r_[0:9, n // 2 - 20:n // 2 + 20, n - 20:n])
         here = torch.from_numpy(picked).cuda()

@@ -137,8 +137,8 @@ def test_kernels_of_the_product(hb, m, n, k, dtype, names):
     (4, 600, 8000, ["gemm_mx4_few_kernel<1, 16, {}, true>"]),
     (1, 40, 32700, ["gemm_mx4_few_kernel<1, 16, {}, true>"]),
     (2, 12300, 8100, ["gemm_mx4_few_kernel<1, 8, {}, true>"]),
-    (9, 1000, 4000, ["quant_mx4_along_kernel<{}, 0>", "gemm_mx4_few_kernel<2, 8, {}, false>"]),
-    (4, 40, 8200, ["quant_mx4_along_kernel<{}, 0>", "gemm_mx4_few_kernel<2, 8, {}, false>"]),
+    (9, 1000, 4000, ["quant_mx4_along_kernel<{}, 0, 1>", "gemm_mx4_few_kernel<2, 8, {}, false>"]),
+    (4, 40, 8200, ["quant_mx4_along_kernel<{}, 0, 1>", "gemm_mx4_few_kernel<2, 8, {}, false>"]),
 ])
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_kernels_of_the_linear_layer(hb, m, n, k, names, dtype):
