@@ -1017,9 +1017,12 @@ def mx4_plan(rows: int, kdim: int) -> Mx4Desc:
     return d
 
 
+_mx4_sizes = functools.lru_cache(maxsize=1024)(mx4_plan)       # (nothing writes to what this returns; a copy of it is 1.3 us less than a new plan)
+
+
 def mx4_alloc(rows: int, kdim: int, device="cuda") -> Mx4:
     """An operand of `rows` rows and a contraction of `kdim` (its contents are whatever the memory holds)."""
-    d = mx4_plan(rows, kdim)
+    d = Mx4Desc.from_buffer_copy(_mx4_sizes(rows, kdim))
     buffer = torch.empty(d.code_bytes + d.scale_bytes, dtype=torch.uint8, device=device)
     d.codes = buffer.data_ptr()
     d.scales = d.codes + d.code_bytes
