@@ -857,7 +857,11 @@ typedef struct hbfp_mx4 {
     uint64_t code_bytes, scale_bytes;
 } hbfp_mx4;
 
-/* hbfp_mx4_plan (host only).  Errors: HBFP_ERR_ARG (null, sizes <= 0 or from 2^31 on). */
+/*
+ * hbfp_mx4_plan (host only).  Errors: HBFP_ERR_ARG (null, sizes <= 0, rows above 0x7fffffff, kdim above 0x7fffff00: with its last group
+ * filled up a contraction stays below 2^31).  The same limits hold wherever a contraction has these sizes: for both sizes of a source
+ * that is converted both ways, and for M, N (rows) and K (kdim) of the products.
+ */
 int hbfp_mx4_plan(int64_t rows, int64_t kdim, hbfp_mx4 *out);
 
 /*
@@ -905,6 +909,7 @@ int hbfp_linear_mx4(const void *x, int dtype, int64_t M, int64_t ldx, const hbfp
  *   rstd     FP32 [rows] or NULL: what hbfp_norm_grad needs
  *   values   NULL, or receives the values that the codes stand for, rounded to the type
  *   eps      finite, above 0
+ *   rows, cols   at most 0x7fffffff and 0x7fffff00, as of every matrix here
  * Otherwise outputs may not overlap inputs or each other (x, residual, sum and values may be columns of one matrix).  A row that holds
  * an Inf or a NaN gets an Inf or NaN as its scale, or as that of at least one block, so that what is multiplied with it is NaN or Inf.
  * Errors: HBFP_ERR_ARG, HBFP_ERR_FORMAT (dtype), HBFP_ERR_LAYOUT (out is not the plan of (rows, cols)), HBFP_ERR_LAUNCH.
