@@ -902,8 +902,9 @@ int hbfp_linear_mx4(const void *x, int dtype, int64_t M, int64_t ldx, const hbfp
  *   rstd = 1 / sqrt(mean over the row of sum^2 + eps)
  *   n    = sum * rstd * weight, in 64 bits, rounded once to FP32 (weight: FP32 [cols] or NULL for ones)
  * hbfp_norm_i8 delivers n as hbfp_quant_rows converts it (codes, scales: the operand of hbfp_gemm_rows), hbfp_norm_mx4 as
- * hbfp_quant_mx4 does, to nearest and along the rows.  Up to the rounding to FP32 everything is held in 64 bits, so that codes do not
- * depend on the order of a sum.
+ * hbfp_quant_mx4 does, to nearest and along the rows.  Up to the rounding to FP32 everything is held in 64 bits, so that codes hardly
+ * ever depend on the order of a sum: another order moves rstd by some 2^-50 of itself and with it the FP32 rounding of one n in 2^26 or
+ * so, and a code only where that n lies at a border.  The order here depends on `cols` alone.
  *   x, residual, sum, values   [rows] rows of `cols`, of one type, with leading dimensions of their own
  *   sum      receives the sum (NULL: it is not stored); may be x or residual, with the same leading dimension
  *   rstd     FP32 [rows] or NULL: what hbfp_norm_grad needs
