@@ -878,7 +878,8 @@ int hbfp_read_mx4(const hbfp_mx4 *t, int dtype, void *dst, int64_t ld, void *str
 
 /*
  * hbfp_gemm_mx4: Y[m][n] = sum_k a[m][k] b[n][k] + bias[n] of the values the operands hold: blocks of 32 exactly, their sums in FP32,
- * Y rounded once to its type.  a: M = a->rows rows, b: N = b->rows rows, equal kdim.  bias: FP32 [N] or NULL.  y: [M][ldy], ldy >= N.
+ * Y rounded once to its type.  Below FP32's normal range sums go in steps of 2^-149: a product smaller than a step may vanish.
+ * a: M = a->rows rows, b: N = b->rows rows, equal kdim.  bias: FP32 [N] or NULL.  y: [M][ldy], ldy >= N.
  * The three products of a linear layer y = x w^T, with x [tokens][in], w [out][in] and dy [tokens][out]:
  *   y = x along . w along;   dx = dy along . w down;   dw = dy down . x down.
  * hbfp_linear_mx4: hbfp_quant_mx4 of x (to nearest, along its rows) and the product in one call; Y has x's type.  Rows of y may not
