@@ -24,7 +24,8 @@ __device__ __forceinline__ v8i four_bit(const v4i &x) { return v8i{x[0], x[1], x
 // Bound by the chip's power and by what a tile has around its loop: 4096^3 on tiles of 256, one round: ring filled after 2.2 us, loop 26 us at
 // 1.64 GHz with the matrix core busy 76 % of it (of the 5.9 PFLOP/s that a register-only loop gets at 1.5 GHz, 5.2), store 6.5 us with all compute
 // units at once: 38.4 us, 3.6 PFLOP/s; 8192^3 248 us, 4.4 PFLOP/s.  With the requests and copies behind whole rows of matrix instructions instead of
-// single ones 8192^3 took 253, with a unit's tiles in one workgroup and copies running on 258 (copies and stores share a counter).
+// single ones 8192^3 took 253, with a unit's tiles in one workgroup and copies running on 258 (copies and stores share a counter).  Tiles of 256 take
+// 252 registers and 256 accumulators; with FP32 outputs one register more is in scratch, around the loop.
 struct Mx4Params {
     Mx4Product q;
     float *partial;              // split along k: FP32 sums [splits][M][N]

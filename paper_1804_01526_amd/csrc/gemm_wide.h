@@ -73,8 +73,8 @@ __device__ __forceinline__ uint16_t half_bits(float x) {
 }
 
 // store_result for 16-bit outputs.  Neighbouring lanes hold neighbouring columns of the same rows: of two rows an even lane
-// takes both columns of the first and an odd lane those of the second, so that a lane stores 32 bits, at addresses that need to be
-// even only (pair; without it one by one).
+// takes both columns of the first and an odd lane those of the second, so that a lane stores 32 bits, inside y and at its edges (pair;
+// without it 16 bits one by one).  The addresses of pairs need to be even only.
 template <int TI, int TJ, int OUT, class V>
 __device__ __forceinline__ void store_result16(uint16_t *dst, int64_t ld, int64_t rows, int64_t cols, bool pair, int lane, const V &value) {
     typedef uint32_t two_at __attribute__((aligned(2)));
@@ -333,6 +333,9 @@ __global__ __launch_bounds__(kWideThreads, T == 4 ? 1 : 2) void gemm_i8_wide_ker
         };
         if constexpr (OUT == kWideF32) store_result<T, T, STREAM>(p.C + i0 * p.ldc + j0, p.ldc, p.M - i0, p.N - j0, false, lane, value);
         else
+            // in pairs where rows of y begin at multiples of 4 bytes (us, bf16, with the edges one by one and in pairs: 4090 x 4090 x 4096 70.9 and 67.6,
+            // 777 x 2730 x 1024 9.6 and 9.2, 3000 x 6000 x 3000 64.5 and 65.1).  Elsewhere one by one, although pairs would be possible and are ahead
+            // there too: 4096 x 4095 x 1024 36.2 and 30.7, 4090 x 4091 x 4096 74.8 and 68.8, 777 x 2731 x 1024 10.3 and 8.9
             store_result16<T, T, OUT>(reinterpret_cast<uint16_t *>(p.C) + i0 * p.ldc + j0, p.ldc, p.M - i0, p.N - j0,
                                       ((uint64_t)(uintptr_t)p.C | (uint64_t)p.ldc * 2) % 4 == 0, lane, value);
         return;

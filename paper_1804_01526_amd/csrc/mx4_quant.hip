@@ -72,7 +72,8 @@ __global__ __launch_bounds__(256) void quant_mx4_along_kernel(const QuantMx4Para
 // ---- down the columns, or both.  A workgroup has a tile of 128 rows and 16 C columns, a thread 8 rows and C columns of it: 32 / C neighbouring lanes
 // share the blocks along its rows, and the four lanes 16 apart of a wave those down its columns, so that both maxima are found between lanes and a random
 // word serves both codes of its value (with values that meet in LDS and are rounded by each side for itself, stochastic 4096 x 4096 took 44 us, 1001 x 777
-// 31 instead of 13).  The words of the columns meet in LDS, from where four threads store 64 bytes of a column's codes.
+// 31 instead of 13).  The words of the columns meet in LDS, from where four threads store 64 bytes of a column's codes.  The writes there are free of
+// conflicts; of the reads, 16 bytes a lane, every fourth row's end meets the banks of the first: 0.57 cycles of conflict for each cycle of an access.
 
 // largest of the lanes l, l ^ 16, l ^ 32, l ^ 48: two exchanges of rows of lanes on the vector unit
 __device__ __forceinline__ uint32_t largest_of_column(uint32_t x) {
@@ -202,7 +203,7 @@ __global__ __launch_bounds__(256, ALONG && ROUND == HBFP_STOCHASTIC && C == 8 ? 
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < (C + 2) / 4; ++i) {
-        const int col = C * (lane / 4) + t / 64 + 4 * i;     // (columns C apart: neighbouring rows of words, every bank once)
+        const int col = C * (lane / 4) + t / 64 + 4 * i;     // (columns C apart: neighbouring rows of words, 20 banks from one to the next)
         if ((C > 2 || t < 128) && c0 + col < p.cols)
             *reinterpret_cast<v4u *>(p.down.codes + (group * p.cols + c0 + col) * 128 + ((r0 & 255) >> 1) + 16 * (t % 4)) =
                 *reinterpret_cast<const v4u *>(&words[16 * (col % C) + col / C][4 * (t % 4)]);
@@ -221,7 +222,8 @@ int launch_down(QuantMx4Params p, bool along, hipStream_t s) {
     return launch_status();
 }
 
-// Rows of a thread, of the kernels that go along the rows: one where they are few, else two.  us with 1, 2 and 4, conversion to nearest and stochastically and
+// Rows of a thread, of the kernels that go along the rows: one where they are few, else two, a compromise between the conversions and reading back: four are
+// ahead to nearest at 4096 x 4096, two at 8192 x 8192 and for reading back from 8192 x 8192 on.  us with 1, 2 and 4, conversion to nearest and stochastically and
 // reading back, of bf16: 64 x 4096 3.1, 3.3, 3.6; 3.4, 3.9, 5.2; 2.9, 3.0, 3.2; 1024 x 1024 (512 workgroups of one row a thread) 3.0, 3.2, 3.7; 4.0, 4.1, 5.3; 3.1,
 // 3.2, 3.5; 512 x 8192 3.9, 3.9, 4.1; 7.9, 6.6, 7.1; 4.3, 4.4, 4.5; 4096 x 4096 9.5, 8.9, 8.2; 23.3, 18.7, 19.5; 8.5, 8.5, 8.4; 8192 x 8192 -, 26.2, 32.0;
 // -, 59.0, 62.2; 26.5, 26.5, 29.0; 16384 x 16384 -, 112, 115; -, 225, 223; 168, 129, 135

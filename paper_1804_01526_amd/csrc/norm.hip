@@ -424,7 +424,7 @@ void launch_grad_rows(const GradParams &p, hipStream_t s) {
 }
 // Eight columns a thread and the next row ahead as far as a workgroup of 16 waves goes.  us (bf16) of 4096 x 4096 on 8 waves 26.9, on 4 with 16
 // columns a thread 32.0, without the next row ahead 27.1 and 32.9; 2048 x 8192 on 16 waves 27.1, on 8 31.3; 1024 x 16384, 16 columns a thread,
-// without the next row ahead 32.4, with it 48.9 (registers in scratch)
+// without the next row ahead 32.4, with it 48.9 (registers in scratch; without it FP32 keeps two there, the 16-bit types none)
 template <int DT>
 int launch_grad(const NormGradArgs &a, hipStream_t s) {
     const GradParams p = {a, (int32_t)grad_wgs(a.rows, a.cols)};
